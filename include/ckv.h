@@ -374,6 +374,147 @@ int ckv_layer_error(const ckv_attn_desc *desc, const void *q, int64_t q_stride_t
  * averaged, the average normalised to sum 1. CKV_OK or CKV_ERR_INVALID_ARG. */
 int ckv_normalize_errors(const double *e, int32_t n_sets, int32_t n_layers, double *e_tilde);
 
+/* ---- attention around the compressed cache -------------------------------
+ * What a serving program runs before and after ckv_compress_layer: the prompt's
+ * own attention, which leaves the window rows' log-sum-exp for the scoring, a
+ * paged cache that takes the compact rows and the tokens after them, and the
+ * attention of new tokens over it. They share ckv_attn_desc; outputs have the
+ * descriptor's dtype, everything accumulates in fp32. Weights of 16-bit types
+ * are rounded once to that type for the product with V, after the maximum (or
+ * a number at most 2^8 below it) was divided out; their sum is taken before.
+ * A NaN or an infinity in a key or value reaches the rows that see it and no
+ * other. All work is asynchronous on stream, makes no allocation, and may be
+ * captured into a graph. */
+
+/* Causal attention of whole prompts, packed one after the other: token t of
+ * prompt i is row cu_seqlens[i] + t of every array, and sees the prompt's
+ * tokens 0..t (paper Eq. 2 over the whole prompt, then its product with V).
+ *   q    row r, head h at q + r * q_stride_tok + h * q_stride_head
+ *   k, v row r, KV head g at k + r * kv_stride_tok + g * kv_stride_head
+ *   out  row r, head h at out + r * out_stride_tok + h * out_stride_head
+ *        (dtype of the descriptor; may not overlap the inputs)
+ *   lse  optional fp32: log-sum-exp (natural log) of row r's scaled logits, at
+ *        lse + h * lse_stride_head + r. The last w values of a prompt, from
+ *        lse + cu_seqlens[i + 1] - w on, are ckv_seq.lse of that prompt.
+ * Strides in elements, d contiguous; pointers but lse 16-byte aligned, strides
+ * but lse's multiples of 16 bytes. */
+typedef struct {
+  const void *q;
+  const void *k;
+  const void *v;
+  void *out;
+  int64_t q_stride_tok, q_stride_head;
+  int64_t kv_stride_tok, kv_stride_head;
+  int64_t out_stride_tok, out_stride_head;
+  float *lse;
+  int64_t lse_stride_head;
+} ckv_packed_attn;
+
+/* cu_seqlens is a host array [num_seqs + 1], cu_seqlens[0] >= 0, not falling
+ * (prompts may be empty), read during the call only. Rows before the first
+ * and behind the last are left as they are. Up to CKV_PREFILL_SEQS prompts go
+ * to the GPU in one launch. */
+#define CKV_PREFILL_SEQS 448
+int ckv_prefill_attention(const ckv_attn_desc *desc, const ckv_packed_attn *a,
+                          const int32_t *cu_seqlens, int32_t num_seqs, void *stream);
+
+/* One layer's paged cache: page p holds tokens p * page_size .. of a pool that
+ * requests share; slot p * page_size + i, KV head g, is the row of d elements
+ * at k + p * stride_page + g * stride_head + i * stride_tok (v alike). Pointers
+ * 16-byte aligned, strides in elements and multiples of 16 bytes. Any
+ * page_size >= 1; n_pages * page_size < 2^31. */
+typedef struct {
+  void *k;
+  void *v;
+  int64_t stride_page, stride_head, stride_tok;
+  int32_t n_pages;
+  int32_t page_size;
+} ckv_paged_cache;
+
+/* Block tables and slot maps of one step, made on the GPU from the requests'
+ * lengths (all arrays int32 device memory). Request s has cached[s] tokens and
+ * takes in add[s] more (negative counts as 0). The pages that it lacks come
+ * from the free list, request after request, in its order:
+ *   table     [num_seqs][table_stride] block tables, table_width entries used.
+ *             Entries of new pages are written, all others left.
+ *   free_pages [n_free]; free_head (optional, one number) pages of it are taken
+ *             already. free_head_out: free_head plus the pages that this step
+ *             needs; more than n_free means that some requests went without.
+ *   cu_q      [num_seqs + 1]: first row of every request's new tokens
+ *   kv_len    [num_seqs]: cached[s] + add[s]
+ *   slots     [n_slots]: the slot of row r of the new tokens, -1 where its page
+ *             is missing (free list at its end, table too narrow, a negative
+ *             entry) and from row cu_q[num_seqs] on.
+ * These are what ckv_paged_write and ckv_paged_attention take. Outputs may not
+ * overlap inputs, nor each other. Sums of lengths stay below 2^31; wrong numbers in
+ * device memory give wrong tables, not accesses outside the arrays. */
+#define CKV_MAX_PAGED_SEQS 4096
+typedef struct {
+  const int32_t *cached;
+  const int32_t *add;
+  int32_t num_seqs;
+  int32_t page_size;
+  int32_t *table;
+  int64_t table_stride;
+  int32_t table_width;
+  int32_t n_free;
+  const int32_t *free_pages;
+  const int32_t *free_head;
+  int32_t *cu_q;
+  int32_t *kv_len;
+  int32_t *slots;
+  int32_t *free_head_out;
+  int32_t n_slots;
+  int32_t reserved;
+} ckv_page_plan;
+
+int ckv_paged_plan(const ckv_page_plan *plan, void *stream);
+
+/* Writes n rows of K and V into the cache: row r of KV head g, at
+ * k + g * stride_head + r * stride_tok (v alike), goes to slot slots[r] (device
+ * int32 [n]). Rows whose slot is negative or past the pool are left out. New
+ * tokens as the projections wrote them and compact caches of
+ * ckv_compress_layer (stride_tok = d, stride_head = min(B, L) * d) both fit. A
+ * slot may occur once among the n. */
+int ckv_paged_write(const ckv_attn_desc *desc, const ckv_paged_cache *cache, const void *k,
+                    const void *v, int64_t stride_tok, int64_t stride_head, const int32_t *slots,
+                    int64_t n, void *stream);
+
+/* Which rows a step brings and which tokens they see (device int32 arrays). The
+ * T = cu_q[s + 1] - cu_q[s] rows from cu_q[s] on are the last T of request s's
+ * kv_len[s] cached tokens (already written): row t sees the tokens
+ * 0 .. kv_len[s] - T + t, the token j at slot
+ * table[s * table_stride + j / page_size] * page_size + j % page_size. Tokens of pages outside
+ * [0, n_pages), or past table_width, count as not there. A row that sees none
+ * gets zeros, and -inf in lse. The bounds size the launch and the workspace, so
+ * a captured graph serves every step within them: no request has more than
+ * max_q rows or max_kv tokens, all together at most total_q rows. Rows from
+ * cu_q[num_seqs] on are left as they are. Wrong numbers in device memory give
+ * wrong results, not accesses outside the arrays. */
+typedef struct {
+  const int32_t *cu_q;
+  const int32_t *kv_len;
+  const int32_t *table;
+  int64_t table_stride;
+  int32_t table_width;
+  int32_t num_seqs;
+  int32_t total_q;
+  int32_t max_q;
+  int32_t max_kv;
+  int32_t reserved;
+} ckv_paged_batch;
+
+/* Workspace of ckv_paged_attention for a batch within these bounds (its device
+ * pointers are not read and may be NULL); 0 on invalid input. */
+size_t ckv_paged_workspace_bytes(const ckv_attn_desc *desc, const ckv_paged_batch *batch);
+
+/* Attention of every row of the batch over its request's cache: single tokens,
+ * a few drafted ones, chunks of a prompt, or a mix. q, out and lse are as in
+ * ckv_packed_attn (its k, v and their strides are not used), rows 0 .. total_q - 1. */
+int ckv_paged_attention(const ckv_attn_desc *desc, const ckv_paged_cache *cache,
+                        const ckv_paged_batch *batch, const ckv_packed_attn *a, void *workspace,
+                        size_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *ckv_status_string(int status);
 

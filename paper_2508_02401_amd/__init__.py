@@ -15,4 +15,7 @@ from ._binding import (  # noqa: F401
     ckv_decode_attention_batch, ckv_streaming_select, snapkv_mask,
     CKV_NOALLOC_MAX_WORKSPACE_BYTES, ckv_compress_layer_noalloc, CKV_STACK_LAYERS_PER_LAUNCH,
     CKV_STACK_CHUNK_TOKENS, stack_layers_per_launch,
+    ckv_prefill_attention, paged_cache, paged_batch, ckv_paged_plan, ckv_paged_write,
+    ckv_paged_workspace_bytes, ckv_paged_attention, ckv_packed_attn, ckv_paged_cache,
+    ckv_page_plan, ckv_paged_batch,
 )

@@ -48,7 +48,9 @@ EXPORTED = ("ckv_workspace_bytes", "ckv_score", "ckv_select", "ckv_gather", "ckv
             "ckv_last_hip_error", "ckv_set_stage_events", "ckv_set_stack_stage_events",
             "ckv_decode_workspace_bytes", "ckv_decode_attention", "ckv_layer_error_workspace_bytes",
             "ckv_layer_error", "ckv_normalize_errors", "ckv_decode_batch_workspace_bytes",
-            "ckv_decode_attention_batch", "ckv_streaming_select", "ckv_compress_layer_noalloc")
+            "ckv_decode_attention_batch", "ckv_streaming_select", "ckv_compress_layer_noalloc",
+            "ckv_prefill_attention", "ckv_paged_plan", "ckv_paged_write",
+            "ckv_paged_workspace_bytes", "ckv_paged_attention")
 
 _DTYPE_CODE = {torch.bfloat16: CKV_BF16, torch.float16: CKV_F16, torch.float32: CKV_F32}
 
@@ -86,6 +88,40 @@ class ckv_decode_seq(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("q_stride_t", ctypes.c_int64),
                 ("q_stride_h", ctypes.c_int64), ("T", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("cache", ckv_kv_cache), ("out", ctypes.c_void_p)]
+
+
+class ckv_packed_attn(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("q_stride_tok", ctypes.c_int64),
+                ("q_stride_head", ctypes.c_int64), ("kv_stride_tok", ctypes.c_int64),
+                ("kv_stride_head", ctypes.c_int64), ("out_stride_tok", ctypes.c_int64),
+                ("out_stride_head", ctypes.c_int64), ("lse", ctypes.c_void_p),
+                ("lse_stride_head", ctypes.c_int64)]
+
+
+class ckv_paged_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("stride_page", ctypes.c_int64),
+                ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class ckv_page_plan(ctypes.Structure):
+    _fields_ = [("cached", ctypes.c_void_p), ("add", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("table_width", ctypes.c_int32), ("n_free", ctypes.c_int32),
+                ("free_pages", ctypes.c_void_p), ("free_head", ctypes.c_void_p),
+                ("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("free_head_out", ctypes.c_void_p), ("n_slots", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class ckv_paged_batch(ctypes.Structure):
+    _fields_ = [("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("table_width", ctypes.c_int32),
+                ("num_seqs", ctypes.c_int32), ("total_q", ctypes.c_int32),
+                ("max_q", ctypes.c_int32), ("max_kv", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class CkvError(RuntimeError):
@@ -141,6 +177,17 @@ def load() -> ctypes.CDLL:
         lib.ckv_decode_batch_workspace_bytes.argtypes = [AD, DS, ctypes.c_int32]
         lib.ckv_decode_batch_workspace_bytes.restype = ctypes.c_size_t
         lib.ckv_decode_attention_batch.argtypes = [AD, DS, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+        i32, i64, PA = ctypes.c_int32, ctypes.c_int64, P(ckv_packed_attn)
+        PC, PB = P(ckv_paged_cache), P(ckv_paged_batch)
+        lib.ckv_prefill_attention.argtypes = [AD, PA, P(i32), i32, vp]
+        lib.ckv_paged_plan.argtypes = [P(ckv_page_plan), vp]
+        lib.ckv_paged_write.argtypes = [AD, PC, vp, vp, i64, i64, vp, i64, vp]
+        lib.ckv_paged_workspace_bytes.argtypes = [AD, PB]
+        lib.ckv_paged_workspace_bytes.restype = ctypes.c_size_t
+        lib.ckv_paged_attention.argtypes = [AD, PC, PB, PA, vp, ctypes.c_size_t, vp]
+        for name in ("ckv_prefill_attention", "ckv_paged_plan", "ckv_paged_write",
+                     "ckv_paged_attention"):
+            getattr(lib, name).restype = ctypes.c_int
         for name in ("ckv_decode_attention", "ckv_layer_error", "ckv_normalize_errors",
                      "ckv_decode_attention_batch", "ckv_streaming_select", "ckv_compress_layer_noalloc"):
             getattr(lib, name).restype = ctypes.c_int
@@ -493,3 +540,185 @@ def ckv_normalize_errors(e) -> np.ndarray:
                                        out.ctypes.data_as(ctypes.POINTER(ctypes.c_double))),
            "ckv_normalize_errors")
     return out
+
+
+# --------------------------------------------------------------------------
+# attention around the compressed cache (prompts, paged cache)
+# --------------------------------------------------------------------------
+def _on_device(what: str, *tensors) -> torch.device:
+    """The one device that the tensors (None entries aside) are on, a GPU."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise ValueError("%s: tensors on %s and %s" % (what, dev, t.device))
+    if dev.type != "cuda":
+        raise ValueError("%s: tensors on %s, not on a GPU" % (what, dev))
+    return dev
+
+
+def _call_on(dev: torch.device, fn, what: str, args, stream) -> None:
+    """fn(*args, stream) with dev as the current device; by default on dev's current stream."""
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return _call_on(dev, fn, what, args, stream)
+    _check(fn(*args, _stream(stream)), what)
+
+
+def _int32(what: str, name: str, t: torch.Tensor, dim: int = 1) -> torch.Tensor:
+    if t.dtype != torch.int32 or t.dim() != dim or (t.numel() > 1 and t.stride(-1) != 1):
+        raise ValueError("%s: %s must be int32 with %d axes, the last contiguous" % (what, name, dim))
+    return t
+
+
+def _rows_arg(what: str, desc: ckv_attn_desc, q: torch.Tensor, out: torch.Tensor,
+              lse: Optional[torch.Tensor]) -> ckv_packed_attn:
+    """q, out [N, H, d] and lse [H, N] as the C struct."""
+    shape = (q.shape[0], desc.num_q_heads, desc.head_dim)
+    if q.shape != shape or out.shape != shape:
+        raise ValueError("%s: q and out must be [N, %d, %d]" % ((what,) + shape[1:]))
+    if _DTYPE_CODE.get(q.dtype) != desc.dtype or out.dtype != q.dtype:
+        raise ValueError("%s: q and out must have the descriptor's dtype" % what)
+    qs, os_ = q.stride(), out.stride()
+    if q.numel() and (qs[2] != 1 or os_[2] != 1):
+        raise ValueError("%s: the last axis of q and out must be contiguous" % what)
+    a = ckv_packed_attn(q.data_ptr(), None, None, out.data_ptr(), qs[0], qs[1], 0, 0, os_[0],
+                        os_[1], None, 0)
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != (shape[1], shape[0]) or \
+                (shape[0] > 1 and lse.stride(1) != 1):
+            raise ValueError("%s: lse must be fp32 [H, N] with N contiguous" % what)
+        a.lse, a.lse_stride_head = lse.data_ptr(), lse.stride(0)
+    return a
+
+
+def _pair(what: str, desc: ckv_attn_desc, k: torch.Tensor, v: torch.Tensor, dims: int) -> None:
+    if k.shape != v.shape or k.stride() != v.stride() or k.dim() != dims or \
+            k.shape[-1] != desc.head_dim or (k.numel() and k.stride(-1) != 1):
+        raise ValueError("%s: k and v must have equal shapes and strides, [.., %d] with the last "
+                         "axis contiguous" % (what, desc.head_dim))
+    if _DTYPE_CODE.get(k.dtype) != desc.dtype or v.dtype != k.dtype:
+        raise ValueError("%s: k and v must have the descriptor's dtype" % what)
+
+
+def ckv_prefill_attention(desc: ckv_attn_desc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                          cu_seqlens: Sequence[int], out: torch.Tensor,
+                          lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention of packed prompts: prompt i's tokens are rows cu_seqlens[i] ..
+    cu_seqlens[i + 1] (host numbers). q, out [N, H, d]; k, v [n_kv, N, d]; lse [H, N] fp32, whose
+    last w columns of a prompt are Seq.lse for its compression."""
+    what = "ckv_prefill_attention"
+    a = _rows_arg(what, desc, q, out, lse)
+    _pair(what, desc, k, v, 3)
+    if k.shape[:2] != (desc.num_kv_heads, q.shape[0]):
+        raise ValueError("%s: k and v must be [n_kv, N, d]" % what)
+    n = len(cu_seqlens) - 1
+    if n < 1 or cu_seqlens[n] > q.shape[0]:
+        raise ValueError("%s: cu_seqlens must hold 2 or more row numbers, none past N" % what)
+    a.k, a.v = k.data_ptr(), v.data_ptr()
+    a.kv_stride_head, a.kv_stride_tok = k.stride(0), k.stride(1)
+    cu = (ctypes.c_int32 * (n + 1))(*cu_seqlens)
+    _call_on(_on_device(what, q, k, v, out, lse), load().ckv_prefill_attention, what,
+             (ctypes.byref(desc), ctypes.byref(a), cu, n), stream)
+
+
+def paged_cache(k: torch.Tensor, v: torch.Tensor) -> ckv_paged_cache:
+    """One layer's paged cache, k and v [n_pages, n_kv, page_size, d] with the same strides (any
+    but the last's: a [n_pages, page_size, n_kv, d] pool is passed transposed)."""
+    if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or \
+            k.stride(3) != 1:
+        raise ValueError("paged_cache: k and v must be [n_pages, n_kv, page_size, d] with equal "
+                         "strides and types, d contiguous")
+    c = ckv_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                        k.shape[0], k.shape[2])
+    c.tensors = (k, v)  # kept alive, and looked at by the calls
+    return c
+
+
+def _cache_arg(what: str, desc: ckv_attn_desc, cache: ckv_paged_cache):
+    k, v = cache.tensors
+    if k.shape[1] != desc.num_kv_heads:
+        raise ValueError("%s: the cache must have the descriptor's KV heads" % what)
+    _pair(what, desc, k, v, 4)
+    return k, v
+
+
+def ckv_paged_plan(cached: torch.Tensor, add: torch.Tensor, table: torch.Tensor, page_size: int,
+                   free_pages: torch.Tensor, free_head: Optional[torch.Tensor], cu_q: torch.Tensor,
+                   kv_len: torch.Tensor, slots: torch.Tensor, free_head_out: torch.Tensor,
+                   stream=None) -> None:
+    """Block tables and slot maps of a step (int32 device tensors, see include/ckv.h): writes
+    table [n, width] (new entries), cu_q [n + 1], kv_len [n], slots [n_slots], free_head_out [1]."""
+    what = "ckv_paged_plan"
+    n = cached.shape[0]
+    for name, t, size in (("cached", cached, n), ("add", add, n), ("cu_q", cu_q, n + 1),
+                          ("kv_len", kv_len, n), ("free_pages", free_pages, None),
+                          ("free_head", free_head, 1), ("slots", slots, None),
+                          ("free_head_out", free_head_out, 1)):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or t.dim() != 1 or
+                              size not in (None, t.shape[0])):
+            raise ValueError("%s: %s must be contiguous int32 [%s]" % (what, name, size or "n"))
+    _int32(what, "table", table, 2)
+    if table.shape[0] != n:
+        raise ValueError("%s: table must be [%d, width]" % (what, n))
+    p = ckv_page_plan(cached.data_ptr(), add.data_ptr(), n, page_size, table.data_ptr(),
+                      table.stride(0), table.shape[1], free_pages.shape[0], free_pages.data_ptr(),
+                      _ptr(free_head), cu_q.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
+                      free_head_out.data_ptr(), slots.shape[0], 0)
+    dev = _on_device(what, cached, add, table, free_pages, free_head, cu_q, kv_len, slots,
+                     free_head_out)
+    _call_on(dev, load().ckv_paged_plan, what, (ctypes.byref(p),), stream)
+
+
+def ckv_paged_write(desc: ckv_attn_desc, cache: ckv_paged_cache, k: torch.Tensor, v: torch.Tensor,
+                    slots: torch.Tensor, stream=None) -> None:
+    """Rows r of k, v [n_kv, n, d] into the cache's slots[r] (int32 [n] or more on the device);
+    rows with a negative slot are left out."""
+    what = "ckv_paged_write"
+    ck, _ = _cache_arg(what, desc, cache)
+    _pair(what, desc, k, v, 3)
+    if k.shape[0] != desc.num_kv_heads:
+        raise ValueError("%s: k and v must be [n_kv, n, d]" % what)
+    _int32(what, "slots", slots)
+    if slots.shape[0] < k.shape[1]:
+        raise ValueError("%s: fewer slots than rows" % what)
+    _call_on(_on_device(what, ck, k, v, slots), load().ckv_paged_write, what,
+             (ctypes.byref(desc), ctypes.byref(cache), k.data_ptr(), v.data_ptr(), k.stride(1),
+              k.stride(0), slots.data_ptr(), k.shape[1]), stream)
+
+
+def paged_batch(cu_q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, total_q: int,
+                max_q: int, max_kv: int) -> ckv_paged_batch:
+    """A step's rows and tables (int32 device tensors cu_q [n + 1], kv_len [n], table [n, width])
+    with the bounds that hold for it."""
+    what = "paged_batch"
+    n = kv_len.shape[0]
+    _int32(what, "cu_q", cu_q), _int32(what, "kv_len", kv_len), _int32(what, "table", table, 2)
+    if cu_q.shape[0] != n + 1 or table.shape[0] != n:
+        raise ValueError("paged_batch: cu_q must be [n + 1] and table [n, width] for kv_len [n]")
+    b = ckv_paged_batch(cu_q.data_ptr(), kv_len.data_ptr(), table.data_ptr(), table.stride(0),
+                        table.shape[1], n, total_q, max_q, max_kv, 0)
+    b.tensors = (cu_q, kv_len, table)
+    return b
+
+
+def ckv_paged_workspace_bytes(desc: ckv_attn_desc, batch: ckv_paged_batch) -> int:
+    return load().ckv_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(batch))
+
+
+def ckv_paged_attention(desc: ckv_attn_desc, cache: ckv_paged_cache, batch: ckv_paged_batch,
+                        q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                        lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of the batch's rows, q and out [N, H, d] (N at least its total_q), lse [H, N]."""
+    what = "ckv_paged_attention"
+    ck, _ = _cache_arg(what, desc, cache)
+    a = _rows_arg(what, desc, q, out, lse)
+    if q.shape[0] < batch.total_q:
+        raise ValueError("%s: fewer rows than total_q" % what)
+    dev = _on_device(what, q, out, ck, workspace, lse, *batch.tensors)
+    _call_on(dev, load().ckv_paged_attention, what,
+             (ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(a),
+              workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)

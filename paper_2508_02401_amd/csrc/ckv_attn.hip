@@ -1,0 +1,507 @@
+// gfx950 (MI355X) attention of whole prompts and of new tokens over a paged
+// cache: out = softmax(scale * Q K^T, causal) V with the rows' log-sum-exp.
+//
+// A workgroup takes a tile of query rows of one KV head g: row r of a request
+// is token r / G, head g * G + r % G, so the G heads that share K and V are
+// neighbouring rows and K and V are read once for all of them. Every wave owns
+// 32 rows and walks the keys tile by tile, all waves together: K and V tiles go
+// from memory straight into LDS (the next tile's while this one is reduced).
+// Per tile: S^T = K Q^T with MFMA, which leaves each query row's logits in two
+// lanes; the running maximum and sum of the softmax; O^T += V^T P^T with MFMA,
+// whose P operand is the lane's own logits in place. V is transposed on the
+// way out of LDS (ds_read_b64_tr_b16).
+#include <math.h>
+
+#include <type_traits>
+
+#include "ckv_device.h"
+
+namespace ckv {
+namespace {
+
+using namespace dev;
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Wait until at most N vector-memory operations of this wave are outstanding
+// and its LDS operations are done; nothing is moved across.
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x070 | (N & 15) | ((N >> 4) << 14));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// exp2 of a logit's distance to the maximum. fp32 keeps weights below 2^-126,
+// which the bare instruction flushes to zero.
+template <int DT>
+__device__ __forceinline__ float weight_exp2(float x) {
+  return DT == 2 ? exp2f(x) : fast_exp2(x);
+}
+
+// Eight fp32 values rounded to the 16-bit operand chunk of an MFMA.
+template <int DT>
+__device__ __forceinline__ uint4 round_chunk(const float* x) {
+  if constexpr (DT == 0) {
+    bf16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
+    return __builtin_bit_cast(uint4, v);
+  } else {
+    f16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (_Float16)x[i];
+    return __builtin_bit_cast(uint4, v);
+  }
+}
+
+// A chunk of V without its values that are not finite, and these in x as numbers
+// that add up without getting mixed over the (at most 64) keys of a tile.
+constexpr float kPlusInf = 1.f, kMinusInf = 128.f, kNan = 16384.f;
+template <int DT>
+__device__ __forceinline__ uint4 strip_chunk(uint4 v, uint4& x) {
+  constexpr uint16_t kExp = DT == 0 ? 0x7F80 : 0x7C00;
+  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+  u16x8 a = __builtin_bit_cast(u16x8, v);
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint16_t mag = a[i] & 0x7FFF;
+    f[i] = mag < kExp ? 0.f : mag > kExp ? kNan : a[i] >> 15 ? kMinusInf : kPlusInf;
+    a[i] = mag < kExp ? a[i] : 0;
+  }
+  x = round_chunk<DT>(f);
+  return __builtin_bit_cast(uint4, a);
+}
+__device__ __forceinline__ float strip_f32(float v, float& x) {
+  x = fabsf(v) < INFINITY ? 0.f : v == INFINITY ? kPlusInf : v == -INFINITY ? kMinusInf : kNan;
+  return fabsf(v) < INFINITY ? v : 0.f;
+}
+// What a sum of such numbers adds to a row's output.
+__device__ __forceinline__ float stripped_sum(float c) {
+  const float minus = floorf(c * (1.f / kMinusInf)) * kMinusInf;
+  const float x = minus == 0.f ? INFINITY : minus == c && c < kNan ? -INFINITY : NAN;
+  return c == 0.f ? 0.f : x;
+}
+// Operand of 8 keys (bits 0..3 and 8..11): 1 for those that the row sees.
+template <int DT>
+__device__ __forceinline__ uint4 seen_chunk(uint32_t bits) {
+  float one[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) one[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? 1.f : 0.f;
+  return round_chunk<DT>(one);
+}
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
+// Four fp32 values to an output row.
+template <int DT>
+__device__ __forceinline__ void store4(char* p, float a, float b, float c, float d) {
+  if constexpr (DT == 2) {
+    *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
+  } else if constexpr (DT == 0) {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
+  } else {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<f16x4*>(p) = f16x4{(_Float16)a, (_Float16)b, (_Float16)c, (_Float16)d};
+  }
+}
+
+// A workgroup's part of the call: T query tokens from row tok0 on that are the
+// last of n keys, KV head g, row tile rt.
+struct Item {
+  int tok0, T, n, g, rt;
+  const int32_t* table;  // paged: the request's block table
+};
+
+__device__ __forceinline__ int clamp_int(int x, int lo, int hi) {
+  return x < lo ? lo : (x > hi ? hi : x);
+}
+
+// Block b of the grid: KV head b % n_kv (neighbouring blocks go to different
+// XCDs, so with 8 KV heads each XCD's L2 holds one head's K and V), row tiles
+// from a prompt's last, longest one on.
+template <int ROWS>
+__device__ __forceinline__ bool find_item(const PrefillArgs& A, Item& it) {
+  const int b = (int)blockIdx.x / A.a.n_kv;
+  it.g = (int)blockIdx.x - b * A.a.n_kv;
+  int lo = 0, hi = A.n;  // the last prompt whose first tile is at most b
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (A.tile[mid] <= b) lo = mid; else hi = mid;
+  }
+  it.tok0 = A.tok[lo];
+  it.T = it.n = A.tok[lo + 1] - it.tok0;
+  it.rt = A.tile[lo + 1] - 1 - b;
+  it.table = nullptr;
+  return true;
+}
+
+// Rows and first row of request s, whatever the device arrays hold.
+__device__ __forceinline__ int request_rows(const PagedArgs& A, int s, int& tok0) {
+  tok0 = clamp_int(A.cu_q[s], 0, A.total_q);
+  const int end = clamp_int(A.cu_q[s + 1], 0, A.total_q);
+  return end > tok0 ? end - tok0 : 0;
+}
+
+template <int ROWS>
+__device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
+  const int b = (int)blockIdx.x / A.a.n_kv;
+  it.g = (int)blockIdx.x - b * A.a.n_kv;
+  const int lane = threadIdx.x & 63;
+  int before = 0;  // row tiles of the requests before s0
+  for (int s0 = 0; s0 < A.num_seqs; s0 += 64) {
+    int tok0 = 0;
+    const int s = s0 + lane;
+    const int T = s < A.num_seqs ? request_rows(A, s, tok0) : 0;
+    const int tiles = (int)(((int64_t)T * A.a.G + ROWS - 1) / ROWS);
+    const int upto = before + (int)wave_incl_scan((uint32_t)tiles);
+    const uint64_t past = __ballot(upto > b);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      it.tok0 = __builtin_amdgcn_readlane(tok0, at);
+      it.T = __builtin_amdgcn_readlane(T, at);
+      it.rt = __builtin_amdgcn_readlane(upto, at) - 1 - b;
+      it.n = __builtin_amdgcn_readfirstlane(clamp_int(A.kv_len[s0 + at], 0, A.max_kv));
+      it.table = A.table + (int64_t)(s0 + at) * A.table_stride;
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
+// How a pass over the tiles treats values that are not finite.
+enum Pass { kPlain, kStripped, kLeftOut };
+
+template <int DT, int D, int NW, bool PAGED, class Args>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2)))
+void attn_kernel(const Args A) {
+  constexpr int EB = Elt<DT>::bytes;
+  constexpr int ROWB = D * EB;            // bytes per K or V row
+  constexpr int NV = ROWB / 16;           // 16-byte chunks per row: 8, 16 or 32
+  constexpr int NC = NV / 2;              // operand chunks per lane
+  constexpr int KT = DT == 2 ? 32 : 64;   // keys per tile
+  constexpr int KB = KT / 32;             // 32-key blocks of it
+  constexpr int VEC = KT * NV;            // 16-byte chunks per tile
+  constexpr int PT = VEC / 64 / NW;       // load instructions per wave and tile, for K and V each
+  constexpr int RPL = 64 / NV;            // tile rows per load instruction
+  constexpr int NB = D / 32;
+  constexpr int ROWS = NW * 32;
+  static_assert(PT >= 1 && VEC % (64 * NW) == 0, "tile loads");
+  constexpr uint64_t kAll = KT == 64 ? ~0ull : 0xFFFFFFFFull;
+  // f16 weights are kept 2^8 larger than exp2(s - max), out of the subnormals
+  // for all but weights below 2^-22; the running maximum is moved when a row
+  // passes it by more than 2^kSlack, so weights stay below 2^14
+  constexpr float kBias = DT == 1 ? 8.f : 0.f;
+  constexpr float kSlack = 6.f;
+  __shared__ uint4 k0[VEC], k1[VEC];  // chunk c of row t at position c ^ swz(t), V's at c ^ vswz(t)
+  __shared__ uint4 v0[VEC], v1[VEC];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Item it;
+  if (!find_item<ROWS>(A, it)) return;
+  const AttnArgs& a = A.a;
+  const int G = a.G, R = it.T * G;
+  // this lane's query row (column of S^T and O^T); row r sees keys 0..limit
+  const int first = it.rt * ROWS + wave * 32;        // of the wave
+  const int shift = it.n - it.T;
+  const bool active = first < R;
+  const int r = first + l32;
+  const bool row_ok = r < R;
+  const int rc = row_ok ? r : R - 1;
+  const int t = rc / G, head = it.g * G + rc - t * G;
+  const int limit = shift + t;
+  const int lim_lo = shift + (active ? first / G : 0);               // the wave's first row's
+  const int lim_hi = active ? shift + (first + 31 < R ? first + 31 : R - 1) / G : -1;
+  const int last_row = it.rt * ROWS + ROWS - 1 < R ? it.rt * ROWS + ROWS - 1 : R - 1;
+  const int keys = shift + last_row / G + 1;         // seen by the tile's last row
+  const int nt = keys > 0 ? (keys + KT - 1) / KT : 0;
+
+  auto swz = [](int row) { return ROWB >= 256 ? (row & 15) : ((row >> 1) & 7); };
+  // V rows of fp32 are read along their columns, which meets every bank as it is
+  auto vswz = [&](int row) { return DT == 2 ? 0 : swz(row); };
+  const int lrow = lane / NV, lpos = lane % NV;
+  const char* kbase = a.k + (int64_t)it.g * a.kv_sh;
+  const char* vbase = a.v + (int64_t)it.g * a.kv_sh;
+  if constexpr (!PAGED) {
+    kbase += (int64_t)it.tok0 * a.kv_st;
+    vbase += (int64_t)it.tok0 * a.kv_st;
+  }
+  // paged: the page of this lane's key of tile tl, -1 for keys that are not there
+  auto page_of = [&](int tl) {
+    int id = -1;
+    if constexpr (PAGED) {
+      const int key = tl * KT + (lane & (KT - 1));
+      if (key < it.n) {
+        const int p = (int)(((uint64_t)(uint32_t)key * A.div.mul) >> A.div.shift);
+        if (p < A.table_width) id = to_global(it.table)[p];
+        if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
+      }
+    }
+    return id;
+  };
+  // the keys of tile tl that are there
+  auto there = [&](int tl, int page) -> uint64_t {
+    if constexpr (PAGED) return __ballot(page >= 0) & kAll;
+    const int left = it.n - tl * KT;
+    return left >= KT ? kAll : (1ull << left) - 1;
+  };
+  // Requests tile tl. Keys that are not there read some valid row.
+  auto fetch = [&](int tl, int page, uint4* ks, uint4* vs) {
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int row = (i * NW + wave) * RPL + lrow;  // of the tile
+      int64_t off;
+      if constexpr (PAGED) {
+        const int key = tl * KT + row;
+        const int id = __shfl(page, row);
+        const int p = (int)(((uint64_t)(uint32_t)key * A.div.mul) >> A.div.shift);
+        const int slot = key - p * A.page_size;
+        off = (int64_t)(id < 0 ? 0 : id) * A.kv_sp + (int64_t)slot * a.kv_st;
+      } else {
+        const int key = tl * KT + row < it.n ? tl * KT + row : it.n - 1;
+        off = (int64_t)key * a.kv_st;
+      }
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(kbase + off + (lpos ^ swz(row)) * 16),
+                                       ks + (i * NW + wave) * 64, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(vbase + off + (lpos ^ vswz(row)) * 16),
+                                       vs + (i * NW + wave) * 64, 16, 0, 0);
+    }
+  };
+
+  // lane half h holds chunks 2c + h of its query row
+  uint4 q[NC];
+  {
+    const CKV_GLOBAL u32x4* src =
+        (const CKV_GLOBAL u32x4*)(to_global(a.q) + (int64_t)(it.tok0 + t) * a.q_st +
+                                  (int64_t)head * a.q_sh) + h;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const u32x4 x = src[2 * c];
+      q[c] = make_uint4(x.x, x.y, x.z, x.w);
+    }
+  }
+  const float alpha = a.alpha;
+  const int i16 = lane & 15;
+  // V^T operand of columns nb * 32 .. + 31 and the 16 keys of MFMA step km: lane i
+  // of a 16-lane group reads columns 4 * (i % 4) .. + 3 of key 8 * jj + 4 * h + i / 4,
+  // and receives column i of the 4 keys
+  auto v_chunk = [&](const char* vt, int nb, int km) {
+    uint2 part[2];
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+      typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+      const int key = 8 * jj + 4 * h + (i16 >> 2);
+      const int col = nb * 32 + (lane & 16) + 4 * (i16 & 3);
+      const int at = key * ROWB + ((col >> 3) ^ vswz(key)) * 16 + (col & 7) * 2;
+      part[jj] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(vt + at + km * 16 * ROWB)));
+    }
+    return make_uint4(part[0].x, part[0].y, part[1].x, part[1].y);
+  };
+  auto v_elem = [&](const char* vt, int nb, int v) {
+    return *reinterpret_cast<const float*>(vt + acc_row(v, h) * ROWB + (nb * 32 + l32) * 4);
+  };
+
+  f32x16 o[NB];
+  float m_run, l_run;
+  // A row's hidden keys have weight 0, but 0 times a value that is not finite
+  // is not 0. If an output came out not finite, the tiles are taken again, first
+  // without such values, then for what every row sees of them.
+  auto pass = [&](auto mode) {
+    constexpr Pass MODE = decltype(mode)::value;
+    if constexpr (MODE != kLeftOut) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) o[nb] = f32x16{};
+      m_run = -INFINITY;
+      l_run = 0.f;
+    }
+    int page = page_of(0);
+    uint64_t seen = nt > 0 ? there(0, page) : 0;
+    if (nt > 0) fetch(0, page, k0, v0);
+    page = page_of(1);
+    auto step = [&](int tl, uint4* ks, uint4* vs, uint4* ks_next, uint4* vs_next) {
+      wait_vm<0>();  // this wave's part of the tile
+      if (seen != kAll) {  // keys that are not there count as zeros in V
+#pragma unroll
+        for (int i = 0; i < PT; ++i) {
+          const int row = (i * NW + wave) * RPL + lrow;
+          if (!((seen >> row) & 1)) vs[(i * NW + wave) * 64 + lane] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        wait_vm<0>();
+      }
+      barrier();
+      const uint64_t vis = seen;
+      if (tl + 1 < nt) {
+        seen = there(tl + 1, page);
+        fetch(tl + 1, page, ks_next, vs_next);
+        page = page_of(tl + 2);
+      }
+      const int j0 = tl * KT;
+      if (!active || j0 > lim_hi) return;
+      // the keys of the tile that this lane's row sees, one bit each
+      const bool hides = vis != kAll || j0 + KT - 1 > lim_lo;
+      uint64_t sees = vis;
+      const int rel = limit - j0;
+      if (hides && rel < KT - 1) sees &= rel < 0 ? 0 : (2ull << rel) - 1;
+      const char* vt = reinterpret_cast<const char*>(vs);
+      if constexpr (MODE == kLeftOut) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          f32x16 c = f32x16{};
+          if constexpr (DT != 2) {
+#pragma unroll
+            for (int km = 0; km < KB * 2; ++km) {
+              uint4 x;
+              strip_chunk<DT>(v_chunk(vt, nb, km), x);
+              c = mfma_chunk<DT>(x, seen_chunk<DT>((uint32_t)(sees >> (16 * km)) >> (4 * h)), c);
+            }
+          } else {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              float x;
+              strip_f32(v_elem(vt, nb, v), x);
+              c = mfma_f32(x, (sees >> acc_row(v, h)) & 1 ? 1.f : 0.f, c);
+            }
+          }
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[nb][v] += stripped_sum(c[v]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        return;
+      }
+      f32x16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        __builtin_amdgcn_sched_barrier(0);
+        s[kb] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          s[kb] = mfma_chunk<DT>(ks[(kb * 32 + l32) * NV + ((2 * c + h) ^ swz(l32))], q[c], s[kb]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if (hides) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) {
+          const uint32_t bits = (uint32_t)(sees >> (32 * kb)) >> (4 * h);
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (!(bits & (1u << acc_row(v, 0)))) s[kb][v] = -INFINITY;
+        }
+      }
+      float mx = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32)) * alpha;
+      if (__any(mx > m_run + kSlack)) {
+        const float m_new = fmaxf(m_run, mx);
+        const float resc = m_run == -INFINITY ? 0.f : weight_exp2<DT>(m_run - m_new);
+        l_run *= resc;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) o[nb] *= resc;
+        m_run = m_new;
+      }
+      const float ms = m_run == -INFINITY ? 0.f : m_run - kBias;
+      float psum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          s[kb][v] = weight_exp2<DT>(fmaf(s[kb][v], alpha, -ms));
+          psum += s[kb][v];
+        }
+      l_run += psum;
+      if constexpr (DT != 2) {
+        // P^T operands: MFMA step km takes this lane's keys acc_row(8km .. 8km+7, h)
+        // = 16km + 4h + (0..3) and 16km + 8 + 4h + (0..3), in that order
+#pragma unroll
+        for (int km = 0; km < KB * 2; ++km) {
+          __builtin_amdgcn_sched_barrier(0);
+          float p[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p[i] = s[km >> 1][8 * (km & 1) + i];
+          const uint4 ph = round_chunk<DT>(p);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            uint4 x, va = v_chunk(vt, nb, km);
+            if constexpr (MODE == kStripped) va = strip_chunk<DT>(va, x);
+            o[nb] = mfma_chunk<DT>(va, ph, o[nb]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          if (v % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            float x, va = v_elem(vt, nb, v);
+            if constexpr (MODE == kStripped) va = strip_f32(va, x);
+            o[nb] = mfma_f32(va, s[0][v], o[nb]);
+          }
+        }
+      }
+    };
+    for (int tl = 0; tl < nt; tl += 2) {
+      step(tl, k0, v0, k1, v1);
+      if (tl + 1 < nt) step(tl + 1, k1, v1, k0, v0);
+    }
+    float bad = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) bad = fmaf(o[nb][v], 0.f, bad);
+    return active && bad != 0.f;
+  };
+  if (__syncthreads_or(pass(std::integral_constant<Pass, kPlain>()))) {
+    pass(std::integral_constant<Pass, kStripped>());
+    __syncthreads();
+    pass(std::integral_constant<Pass, kLeftOut>());
+  }
+  if (!row_ok) return;
+  const float l = l_run + __shfl_xor(l_run, 32);
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+  char* dst = a.out + (int64_t)(it.tok0 + t) * a.o_st + (int64_t)head * a.o_sh;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      store4<DT>(dst + (nb * 32 + acc_row(v, h)) * EB, o[nb][v] * inv, o[nb][v + 1] * inv,
+                 o[nb][v + 2] * inv, o[nb][v + 3] * inv);
+  if (a.lse && h == 0)
+    a.lse[(int64_t)head * a.lse_sh + it.tok0 + t] =
+        l > 0.f ? (float)(((m_run - kBias) + log2f(l)) * 0.6931471805599453) : l == 0.f ? -INFINITY : NAN;
+}
+
+template <bool PAGED, class Args>
+hipError_t launch_attn(int dtype, int d, const Args& A, int grid, hipStream_t st) {
+  if (grid == 0) return hipSuccess;
+  const Timing none;
+  if (d == 128) {
+    if (dtype == CKV_BF16) return launch(attn_kernel<0, 128, 8, PAGED, Args>, grid, 512, st, none, A);
+    if (dtype == CKV_F16) return launch(attn_kernel<1, 128, 8, PAGED, Args>, grid, 512, st, none, A);
+    return launch(attn_kernel<2, 128, 8, PAGED, Args>, grid, 512, st, none, A);
+  }
+  if (dtype == CKV_BF16) return launch(attn_kernel<0, 64, 8, PAGED, Args>, grid, 512, st, none, A);
+  if (dtype == CKV_F16) return launch(attn_kernel<1, 64, 8, PAGED, Args>, grid, 512, st, none, A);
+  return launch(attn_kernel<2, 64, 8, PAGED, Args>, grid, 512, st, none, A);
+}
+
+}  // namespace
+
+hipError_t launch_prefill(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st) {
+  return launch_attn<false>(dtype, d, p, grid, st);
+}
+hipError_t launch_paged(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st) {
+  return launch_attn<true>(dtype, d, p, grid, st);
+}
+
+}  // namespace ckv

@@ -287,4 +287,71 @@ hipError_t launch_select_parts(const LayerArgs& a, const UnitParts& p, hipStream
 // Gather of every layer of a batch: per_layer = the largest per-layer gather grid.
 hipError_t launch_gather_layers(const MultiArgs& m, hipStream_t st, const Timing& tm);
 
+// ---- attention of packed prompts and over a paged cache ----------------------
+// What both read: query rows, outputs, and where K and V rows lie.
+struct AttnArgs {
+  const char* q;
+  const char* k;
+  const char* v;
+  char* out;
+  float* lse;                 // [H][rows], or null
+  int64_t q_st, q_sh;         // bytes
+  int64_t o_st, o_sh;         // bytes
+  int64_t kv_st, kv_sh;       // bytes: token (or slot of a page), head
+  int64_t lse_sh;             // elements
+  int32_t H, n_kv, G;
+  float alpha;                // logit scale * log2(e)
+};
+
+constexpr int kAttnRows = 256;  // query rows of a KV head per workgroup
+
+// Packed prompts: prompt i's rows are tok[i] .. tok[i + 1], its row tiles (per
+// KV head) tile[i] .. tile[i + 1].
+constexpr int kPrefillSeqs = CKV_PREFILL_SEQS;
+struct PrefillArgs {
+  AttnArgs a;
+  int32_t n;
+  int32_t tok[kPrefillSeqs + 1];
+  int32_t tile[kPrefillSeqs + 1];
+};
+static_assert(sizeof(PrefillArgs) <= 4096, "prompts travel as kernel arguments");
+
+struct PagedArgs {
+  AttnArgs a;
+  int64_t kv_sp;              // bytes: page
+  const int32_t* cu_q;
+  const int32_t* kv_len;
+  const int32_t* table;
+  int64_t table_stride;
+  int32_t table_width;
+  int32_t num_seqs;
+  int32_t total_q, max_kv;
+  int32_t n_pages, page_size;
+  PageDiv div;
+};
+
+struct PageWriteArgs {
+  const char* k;
+  const char* v;
+  int64_t st, sh;             // bytes
+  char* ck;
+  char* cv;
+  int64_t sp, csh, cst;       // bytes: page, head, slot
+  const int32_t* slots;
+  int64_t n;
+  int32_t n_kv, row_bytes;
+  int32_t n_pages, page_size;
+  PageDiv div;
+};
+
+struct PagePlanArgs {
+  ckv_page_plan p;
+  PageDiv div;
+};
+
+hipError_t launch_prefill(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st);
+hipError_t launch_paged(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
+hipError_t launch_page_write(const PageWriteArgs& w, hipStream_t st);
+hipError_t launch_page_plan(const PagePlanArgs& p, hipStream_t st);
+
 }  // namespace ckv

@@ -142,4 +142,18 @@ inline int64_t deal_unit_parts(int64_t cus, int32_t num_seqs, int32_t n_sg, int3
   return most;
 }
 
+// Division of a token number (below 2^31) by the page size, as one multiply and
+// shift: with 2^(s-1) < size <= 2^s and mul = ceil(2^(31+s) / size), the error
+// mul * size - 2^(31+s) is below 2^s, so (x * mul) >> (31+s) is exact.
+struct PageDiv {
+  uint32_t mul;
+  int32_t shift;
+};
+inline PageDiv page_div(int32_t size) {
+  int s = 0;
+  while (((int64_t)1 << s) < size) ++s;
+  const uint64_t num = (uint64_t)1 << (31 + s);
+  return PageDiv{(uint32_t)((num + size - 1) / size), 31 + s};
+}
+
 }  // namespace ckv
