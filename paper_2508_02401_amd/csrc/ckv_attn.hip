@@ -14,116 +14,21 @@
 
 #include <type_traits>
 
-#include "ckv_device.h"
+#include "ckv_attn_device.h"
 
 namespace ckv {
 namespace {
 
 using namespace dev;
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-
-// Wait until at most N vector-memory operations of this wave are outstanding
-// and its LDS operations are done; nothing is moved across.
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x070 | (N & 15) | ((N >> 4) << 14));
-  asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void barrier() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-// exp2 of a logit's distance to the maximum. fp32 keeps weights below 2^-126,
-// which the bare instruction flushes to zero.
-template <int DT>
-__device__ __forceinline__ float weight_exp2(float x) {
-  return DT == 2 ? exp2f(x) : fast_exp2(x);
-}
-
-// Eight fp32 values rounded to the 16-bit operand chunk of an MFMA.
-template <int DT>
-__device__ __forceinline__ uint4 round_chunk(const float* x) {
-  if constexpr (DT == 0) {
-    bf16x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (__bf16)x[i];
-    return __builtin_bit_cast(uint4, v);
-  } else {
-    f16x8 v;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (_Float16)x[i];
-    return __builtin_bit_cast(uint4, v);
-  }
-}
-
-// A chunk of V without its values that are not finite, and these in x as numbers
-// that add up without getting mixed over the (at most 64) keys of a tile.
-constexpr float kPlusInf = 1.f, kMinusInf = 128.f, kNan = 16384.f;
-template <int DT>
-__device__ __forceinline__ uint4 strip_chunk(uint4 v, uint4& x) {
-  constexpr uint16_t kExp = DT == 0 ? 0x7F80 : 0x7C00;
-  typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
-  u16x8 a = __builtin_bit_cast(u16x8, v);
-  float f[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint16_t mag = a[i] & 0x7FFF;
-    f[i] = mag < kExp ? 0.f : mag > kExp ? kNan : a[i] >> 15 ? kMinusInf : kPlusInf;
-    a[i] = mag < kExp ? a[i] : 0;
-  }
-  x = round_chunk<DT>(f);
-  return __builtin_bit_cast(uint4, a);
-}
-__device__ __forceinline__ float strip_f32(float v, float& x) {
-  x = fabsf(v) < INFINITY ? 0.f : v == INFINITY ? kPlusInf : v == -INFINITY ? kMinusInf : kNan;
-  return fabsf(v) < INFINITY ? v : 0.f;
-}
-// What a sum of such numbers adds to a row's output.
-__device__ __forceinline__ float stripped_sum(float c) {
-  const float minus = floorf(c * (1.f / kMinusInf)) * kMinusInf;
-  const float x = minus == 0.f ? INFINITY : minus == c && c < kNan ? -INFINITY : NAN;
-  return c == 0.f ? 0.f : x;
-}
-// Operand of 8 keys (bits 0..3 and 8..11): 1 for those that the row sees.
-template <int DT>
-__device__ __forceinline__ uint4 seen_chunk(uint32_t bits) {
-  float one[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) one[i] = bits & (1u << (8 * (i >> 2) + (i & 3))) ? 1.f : 0.f;
-  return round_chunk<DT>(one);
-}
-__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
-}
-
-// Four fp32 values to an output row.
-template <int DT>
-__device__ __forceinline__ void store4(char* p, float a, float b, float c, float d) {
-  if constexpr (DT == 2) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
-  } else if constexpr (DT == 0) {
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)a, (__bf16)b, (__bf16)c, (__bf16)d};
-  } else {
-    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<f16x4*>(p) = f16x4{(_Float16)a, (_Float16)b, (_Float16)c, (_Float16)d};
-  }
-}
-
 // A workgroup's part of the call: T query tokens from row tok0 on that are the
 // last of n keys, KV head g, row tile rt.
 struct Item {
   int tok0, T, n, g, rt;
+  int j0, j1;            // its keys of the n: all, or a chunk
+  int slot;              // where its partial result goes, -1 where the keys are not split
   const int32_t* table;  // paged: the request's block table
 };
-
-__device__ __forceinline__ int clamp_int(int x, int lo, int hi) {
-  return x < lo ? lo : (x > hi ? hi : x);
-}
 
 // Block b of the grid: KV head b % n_kv (neighbouring blocks go to different
 // XCDs, so with 8 KV heads each XCD's L2 holds one head's K and V), row tiles
@@ -140,42 +45,38 @@ __device__ __forceinline__ bool find_item(const PrefillArgs& A, Item& it) {
   it.tok0 = A.tok[lo];
   it.T = it.n = A.tok[lo + 1] - it.tok0;
   it.rt = A.tile[lo + 1] - 1 - b;
+  it.j0 = 0;
+  it.j1 = it.n;
+  it.slot = -1;
   it.table = nullptr;
   return true;
 }
 
-// Rows and first row of request s, whatever the device arrays hold.
-__device__ __forceinline__ int request_rows(const PagedArgs& A, int s, int& tok0) {
-  tok0 = clamp_int(A.cu_q[s], 0, A.total_q);
-  const int end = clamp_int(A.cu_q[s + 1], 0, A.total_q);
-  return end > tok0 ? end - tok0 : 0;
-}
-
 template <int ROWS>
 __device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
+  static_assert(ROWS == kAttnRows, "tiles as paged_cut counts them");
+  __shared__ int64_t part[ROWS / 32];
   const int b = (int)blockIdx.x / A.a.n_kv;
   it.g = (int)blockIdx.x - b * A.a.n_kv;
-  const int lane = threadIdx.x & 63;
-  int before = 0;  // row tiles of the requests before s0
-  for (int s0 = 0; s0 < A.num_seqs; s0 += 64) {
-    int tok0 = 0;
-    const int s = s0 + lane;
-    const int T = s < A.num_seqs ? request_rows(A, s, tok0) : 0;
-    const int tiles = (int)(((int64_t)T * A.a.G + ROWS - 1) / ROWS);
-    const int upto = before + (int)wave_incl_scan((uint32_t)tiles);
-    const uint64_t past = __ballot(upto > b);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      it.tok0 = __builtin_amdgcn_readlane(tok0, at);
-      it.T = __builtin_amdgcn_readlane(T, at);
-      it.rt = __builtin_amdgcn_readlane(upto, at) - 1 - b;
-      it.n = __builtin_amdgcn_readfirstlane(clamp_int(A.kv_len[s0 + at], 0, A.max_kv));
-      it.table = A.table + (int64_t)(s0 + at) * A.table_stride;
-      return true;
-    }
-    before = __builtin_amdgcn_readlane(upto, 63);
-  }
-  return false;
+  const int chunk = paged_cut<ROWS * 2>(A, part).many;
+  auto tiles = [&](const PagedSeq& q) { return (q.T * A.a.G + ROWS - 1) / ROWS; };
+  Found f;
+  if (!find_entry<ROWS * 2>(A, b, [&](const PagedSeq& q) {
+        const bool mine = q.T > 0 && !paged_few(A, q);
+        return make_uint2(mine ? (uint32_t)(tiles(q) * paged_chunks(q.n, chunk)) : 0u, 0u);
+      }, f))
+    return false;
+  const PagedSeq q = paged_seq(A, f.s);
+  const int n_chunks = paged_chunks(q.n, chunk), back = f.within / n_chunks, c = f.within - back * n_chunks;
+  it.tok0 = q.tok0;
+  it.T = q.T;
+  it.n = q.n;
+  it.rt = tiles(q) - 1 - back;
+  it.j0 = c * chunk;
+  it.j1 = n_chunks == 1 || q.n - it.j0 < chunk ? q.n : it.j0 + chunk;
+  it.slot = n_chunks > 1 ? (int)blockIdx.x : -1;
+  it.table = A.table + (int64_t)f.s * A.table_stride;
+  return true;
 }
 
 // How a pass over the tiles treats values that are not finite.
@@ -197,11 +98,7 @@ void attn_kernel(const Args A) {
   constexpr int ROWS = NW * 32;
   static_assert(PT >= 1 && VEC % (64 * NW) == 0, "tile loads");
   constexpr uint64_t kAll = KT == 64 ? ~0ull : 0xFFFFFFFFull;
-  // f16 weights are kept 2^8 larger than exp2(s - max), out of the subnormals
-  // for all but weights below 2^-22; the running maximum is moved when a row
-  // passes it by more than 2^kSlack, so weights stay below 2^14
-  constexpr float kBias = DT == 1 ? 8.f : 0.f;
-  constexpr float kSlack = 6.f;
+  constexpr float kBias = DT == 1 ? kF16Bias : 0.f;
   __shared__ uint4 k0[VEC], k1[VEC];  // chunk c of row t at position c ^ swz(t), V's at c ^ vswz(t)
   __shared__ uint4 v0[VEC], v1[VEC];
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
@@ -222,8 +119,9 @@ void attn_kernel(const Args A) {
   const int lim_lo = shift + (active ? first / G : 0);               // the wave's first row's
   const int lim_hi = active ? shift + (first + 31 < R ? first + 31 : R - 1) / G : -1;
   const int last_row = it.rt * ROWS + ROWS - 1 < R ? it.rt * ROWS + ROWS - 1 : R - 1;
-  const int keys = shift + last_row / G + 1;         // seen by the tile's last row
-  const int nt = keys > 0 ? (keys + KT - 1) / KT : 0;
+  const int keys = min(shift + last_row / G + 1, it.j1);  // seen by the tile's last row
+  const int tl0 = it.j0 / KT;                        // chunks are whole tiles
+  const int nt = keys > it.j0 ? (keys + KT - 1) / KT : tl0;
 
   auto swz = [](int row) { return ROWB >= 256 ? (row & 15) : ((row >> 1) & 7); };
   // V rows of fp32 are read along their columns, which meets every bank as it is
@@ -240,8 +138,8 @@ void attn_kernel(const Args A) {
     int id = -1;
     if constexpr (PAGED) {
       const int key = tl * KT + (lane & (KT - 1));
-      if (key < it.n) {
-        const int p = (int)(((uint64_t)(uint32_t)key * A.div.mul) >> A.div.shift);
+      if (key < it.j1) {
+        const int p = page_at(A.div, key);
         if (p < A.table_width) id = to_global(it.table)[p];
         if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
       }
@@ -263,7 +161,7 @@ void attn_kernel(const Args A) {
       if constexpr (PAGED) {
         const int key = tl * KT + row;
         const int id = __shfl(page, row);
-        const int p = (int)(((uint64_t)(uint32_t)key * A.div.mul) >> A.div.shift);
+        const int p = page_at(A.div, key);
         const int slot = key - p * A.page_size;
         off = (int64_t)(id < 0 ? 0 : id) * A.kv_sp + (int64_t)slot * a.kv_st;
       } else {
@@ -323,10 +221,10 @@ void attn_kernel(const Args A) {
       m_run = -INFINITY;
       l_run = 0.f;
     }
-    int page = page_of(0);
-    uint64_t seen = nt > 0 ? there(0, page) : 0;
-    if (nt > 0) fetch(0, page, k0, v0);
-    page = page_of(1);
+    int page = page_of(tl0);
+    uint64_t seen = nt > tl0 ? there(tl0, page) : 0;
+    if (nt > tl0) fetch(tl0, page, k0, v0);
+    page = page_of(tl0 + 1);
     auto step = [&](int tl, uint4* ks, uint4* vs, uint4* ks_next, uint4* vs_next) {
       wait_vm<0>();  // this wave's part of the tile
       if (seen != kAll) {  // keys that are not there count as zeros in V
@@ -450,7 +348,7 @@ void attn_kernel(const Args A) {
         }
       }
     };
-    for (int tl = 0; tl < nt; tl += 2) {
+    for (int tl = tl0; tl < nt; tl += 2) {
       step(tl, k0, v0, k1, v1);
       if (tl + 1 < nt) step(tl + 1, k1, v1, k0, v0);
     }
@@ -468,7 +366,21 @@ void attn_kernel(const Args A) {
   }
   if (!row_ok) return;
   const float l = l_run + __shfl_xor(l_run, 32);
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+  if constexpr (PAGED) {
+    if (it.slot >= 0) {
+      const int row = wave * 32 + l32;
+      float* orow = partial_o(A.part_many, it.slot, ROWS, D) + row * D;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+          *reinterpret_cast<f32x4*>(orow + nb * 32 + acc_row(v, h)) =
+              f32x4{o[nb][v], o[nb][v + 1], o[nb][v + 2], o[nb][v + 3]};
+      if (h == 0) partial_ml(A.part_many, it.slot, ROWS, D)[row] = make_float2(m_run - kBias, l);
+      return;
+    }
+  }
+  const float inv = row_scale(l);
   char* dst = a.out + (int64_t)(it.tok0 + t) * a.o_st + (int64_t)head * a.o_sh;
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb)
@@ -476,9 +388,7 @@ void attn_kernel(const Args A) {
     for (int v = 0; v < 16; v += 4)
       store4<DT>(dst + (nb * 32 + acc_row(v, h)) * EB, o[nb][v] * inv, o[nb][v + 1] * inv,
                  o[nb][v + 2] * inv, o[nb][v + 3] * inv);
-  if (a.lse && h == 0)
-    a.lse[(int64_t)head * a.lse_sh + it.tok0 + t] =
-        l > 0.f ? (float)(((m_run - kBias) + log2f(l)) * 0.6931471805599453) : l == 0.f ? -INFINITY : NAN;
+  if (a.lse && h == 0) a.lse[(int64_t)head * a.lse_sh + it.tok0 + t] = row_lse(m_run - kBias, l);
 }
 
 template <bool PAGED, class Args>
@@ -500,7 +410,7 @@ hipError_t launch_attn(int dtype, int d, const Args& A, int grid, hipStream_t st
 hipError_t launch_prefill(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st) {
   return launch_attn<false>(dtype, d, p, grid, st);
 }
-hipError_t launch_paged(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st) {
+hipError_t launch_paged_many(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st) {
   return launch_attn<true>(dtype, d, p, grid, st);
 }
 

@@ -86,6 +86,25 @@ int check_batch(const ckv_attn_desc* d, const ckv_paged_batch* b) {
   return CKV_OK;
 }
 
+// Workgroups of one round of the kernel for few rows: two on a CU, one in fp32.
+int32_t few_target(const ckv_attn_desc* d) {
+  return ckv::kCUs * ckv::decode_wgs_per_cu(d->dtype == CKV_F32, d->head_dim, ckv::kFewRows);
+}
+constexpr int32_t kManyTarget = ckv::kCUs;  // and of the tile kernel
+
+// Bytes of the partial results that the kernel for few rows may leave (at most
+// two rounds of slots are split, see paged_share), and the tile kernel (one).
+size_t few_bytes(const ckv_attn_desc* d, const ckv_paged_batch* b) {
+  const int64_t rows = (int64_t)b->max_q * (d->num_q_heads / d->num_kv_heads);
+  if (b->max_kv <= ckv::kFewLeast) return 0;
+  return (size_t)2 * few_target(d) * (rows < ckv::kFewRows ? rows : ckv::kFewRows) * (d->head_dim + 2) * sizeof(float);
+}
+size_t many_bytes(const ckv_attn_desc* d, const ckv_paged_batch* b) {
+  const int64_t rows = (int64_t)b->max_q * (d->num_q_heads / d->num_kv_heads);
+  if (rows <= ckv::kFewRows || b->max_kv <= ckv::kManyLeast) return 0;
+  return (size_t)kManyTarget * ckv::kAttnRows * (d->head_dim + 2) * sizeof(float);
+}
+
 // Whether [a, a + n) and [b, b + m) (numbers of int32) share an element.
 bool overlap(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
   return a && b && (uintptr_t)a < (uintptr_t)(b + m) && (uintptr_t)b < (uintptr_t)(a + n);
@@ -197,7 +216,7 @@ int ckv_paged_write(const ckv_attn_desc* desc, const ckv_paged_cache* cache, con
 
 size_t ckv_paged_workspace_bytes(const ckv_attn_desc* desc, const ckv_paged_batch* batch) {
   if (check_desc(desc) != CKV_OK || check_batch(desc, batch) != CKV_OK) return 0;
-  return 256;
+  return few_bytes(desc, batch) + many_bytes(desc, batch) + 256;
 }
 
 int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
@@ -235,13 +254,43 @@ int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
   p.n_pages = cache->n_pages;
   p.page_size = cache->page_size;
   p.div = ckv::page_div(cache->page_size);
-  // requests' tiles: whole ones of all rows, and one more each for what is left
-  const int64_t G = desc->num_q_heads / desc->num_kv_heads;
-  int64_t tiles = batch->total_q * G / ckv::kAttnRows + batch->num_seqs;
-  const int64_t most = batch->num_seqs * ceil_div(batch->max_q * G, ckv::kAttnRows);
-  if (most < tiles) tiles = most;
-  return status(ckv::launch_paged(desc->dtype, desc->head_dim, p, (int)(tiles * desc->num_kv_heads),
-                                  (hipStream_t)stream));
+  p.part = static_cast<float*>(workspace);
+  p.part_many = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_bytes(desc, batch));
+  // Requests of few and of many rows have a kernel each; one request with many
+  // takes the latter whatever its rows turn out to be
+  const int64_t N = batch->num_seqs, n_kv = desc->num_kv_heads, G = desc->num_q_heads / n_kv;
+  const int64_t most = batch->max_q * G;  // rows of a request and KV head
+  p.has_many = most > ckv::kFewRows;
+  p.few_rows = !p.has_many ? (int32_t)most : N > 1 ? ckv::kFewRows : 0;
+  p.few_target = few_target(desc);
+  p.many_target = kManyTarget;
+  const hipStream_t st = (hipStream_t)stream;
+  hipError_t e = hipSuccess;
+  int64_t merge = 0;
+  if (p.has_many) {
+    // row tiles: whole ones of all rows, and one more each for what is left
+    int64_t tiles = batch->total_q * G / ckv::kAttnRows + N;
+    if (N * ceil_div(most, ckv::kAttnRows) < tiles) tiles = N * ceil_div(most, ckv::kAttnRows);
+    int64_t split = tiles * n_kv * ceil_div(batch->max_kv, ckv::kManyLeast);
+    if (split > p.many_target) split = p.many_target;
+    const int64_t grid = split > tiles * n_kv ? split : tiles * n_kv;
+    if ((e = ckv::launch_paged_many(desc->dtype, desc->head_dim, p, (int)grid, st)) != hipSuccess) return status(e);
+    if (batch->max_kv > ckv::kManyLeast)  // at least two slots per split tile
+      merge += p.many_target / 2 * ckv::kAttnRows / ckv::paged_merge_rows(desc->head_dim);
+  }
+  if (p.few_rows > 0) {
+    int64_t grid = N * n_kv + p.few_target;
+    if (N * n_kv * ceil_div(batch->max_kv, ckv::kFewLeast) < grid)
+      grid = N * n_kv * ceil_div(batch->max_kv, ckv::kFewLeast);
+    if (grid < N * n_kv) grid = N * n_kv;
+    if ((e = ckv::launch_paged_few(desc->dtype, desc->head_dim, p, (int)grid, st)) != hipSuccess) return status(e);
+    if (batch->max_kv > ckv::kFewLeast) {
+      // at least two of the slots per split request and KV head
+      const int64_t by_slots = (int64_t)p.few_target * p.few_rows, by_rows = (int64_t)batch->total_q * desc->num_q_heads;
+      merge += by_slots < by_rows ? by_slots : by_rows;
+    }
+  }
+  return status(ckv::launch_paged_merge(desc->dtype, desc->head_dim, p, (int)merge, st));
 }
 
 }  // extern "C"

@@ -328,7 +328,15 @@ struct PagedArgs {
   int32_t total_q, max_kv;
   int32_t n_pages, page_size;
   PageDiv div;
+  float* part;                // partial results of split requests: the few kernel's slots,
+  float* part_many;           // and the tile kernel's
+  int32_t few_rows;           // requests of up to this many rows per KV head go to the few kernel
+  int32_t has_many;           // the tile kernel is launched
+  int32_t few_target, many_target;  // workgroups in one round
 };
+constexpr int kFewRows = 32;     // rows per KV head of the kernel for few
+constexpr int kFewLeast = 128;   // keys per workgroup, at least
+constexpr int kManyLeast = 1024;
 
 struct PageWriteArgs {
   const char* k;
@@ -350,7 +358,12 @@ struct PagePlanArgs {
 };
 
 hipError_t launch_prefill(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st);
-hipError_t launch_paged(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
+hipError_t launch_paged_many(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
+hipError_t launch_paged_few(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
+// Joins what the two left in parts: a workgroup per row of the few kernel's split
+// requests, one per paged_merge_rows(d) rows of the tile kernel's.
+hipError_t launch_paged_merge(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
+inline int paged_merge_rows(int d) { return 1024 / d; }
 hipError_t launch_page_write(const PageWriteArgs& w, hipStream_t st);
 hipError_t launch_page_plan(const PagePlanArgs& p, hipStream_t st);
 

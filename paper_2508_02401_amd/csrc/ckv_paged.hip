@@ -1,15 +1,11 @@
 // gfx950 (MI355X) kernels that keep a paged KV cache: block tables and slot
 // maps of a step from its requests' lengths, and K/V rows into their slots.
-#include "ckv_device.h"
+#include "ckv_attn_device.h"
 
 namespace ckv {
 namespace {
 
 using namespace dev;
-
-__device__ __forceinline__ int page_at(const PageDiv& d, int x) {
-  return (int)(((uint64_t)(uint32_t)x * d.mul) >> d.shift);
-}
 
 // Pages that hold x tokens, at most `width`.
 __device__ __forceinline__ int pages_of(const PageDiv& d, int size, int x, int width) {
