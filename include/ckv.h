@@ -414,7 +414,7 @@ typedef struct {
  * (prompts may be empty), read during the call only. Rows before the first
  * and behind the last are left as they are. Up to CKV_PREFILL_SEQS prompts go
  * to the GPU in one launch. */
-#define CKV_PREFILL_SEQS 448
+#define CKV_PREFILL_SEQS 240
 int ckv_prefill_attention(const ckv_attn_desc *desc, const ckv_packed_attn *a,
                           const int32_t *cu_seqlens, int32_t num_seqs, void *stream);
 
@@ -449,6 +449,7 @@ typedef struct {
  * overlap inputs, nor each other. Sums of lengths stay below 2^31; wrong numbers in
  * device memory give wrong tables, not accesses outside the arrays. */
 #define CKV_MAX_PAGED_SEQS 4096
+#define CKV_MAX_PAGED_KV 0x7FFFF000
 typedef struct {
   const int32_t *cached;
   const int32_t *add;
@@ -488,7 +489,7 @@ int ckv_paged_write(const ckv_attn_desc *desc, const ckv_paged_cache *cache, con
  * [0, n_pages), or past table_width, count as not there. A row that sees none
  * gets zeros, and -inf in lse. The bounds size the launch and the workspace, so
  * a captured graph serves every step within them: no request has more than
- * max_q rows or max_kv tokens, all together at most total_q rows. Rows from
+ * max_q rows or max_kv (at most CKV_MAX_PAGED_KV) tokens, all together at most total_q rows. Rows from
  * cu_q[num_seqs] on are left as they are. Wrong numbers in device memory give
  * wrong results, not accesses outside the arrays. */
 typedef struct {

@@ -27,27 +27,21 @@ struct Item {
   int tok0, T, n, g, rt;
   int j0, j1;            // its keys of the n: all, or a chunk
   int slot;              // where its partial result goes, -1 where the keys are not split
+  int n_chunks;
   const int32_t* table;  // paged: the request's block table
 };
 
-// Block b of the grid: KV head b % n_kv (neighbouring blocks go to different
-// XCDs, so with 8 KV heads each XCD's L2 holds one head's K and V), row tiles
-// from a prompt's last, longest one on.
 template <int ROWS>
 __device__ __forceinline__ bool find_item(const PrefillArgs& A, Item& it) {
-  const int b = (int)blockIdx.x / A.a.n_kv;
-  it.g = (int)blockIdx.x - b * A.a.n_kv;
-  int lo = 0, hi = A.n;  // the last prompt whose first tile is at most b
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (A.tile[mid] <= b) lo = mid; else hi = mid;
-  }
-  it.tok0 = A.tok[lo];
-  it.T = it.n = A.tok[lo + 1] - it.tok0;
-  it.rt = A.tile[lo + 1] - 1 - b;
+  const PromptTile p = prompt_tile(A);
+  it.tok0 = p.tok0;
+  it.T = it.n = p.T;
+  it.g = p.g;
+  it.rt = p.rt;
   it.j0 = 0;
   it.j1 = it.n;
   it.slot = -1;
+  it.n_chunks = 1;
   it.table = nullptr;
   return true;
 }
@@ -55,18 +49,17 @@ __device__ __forceinline__ bool find_item(const PrefillArgs& A, Item& it) {
 template <int ROWS>
 __device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
   static_assert(ROWS == kAttnRows, "tiles as paged_cut counts them");
-  __shared__ int64_t part[ROWS / 32];
   const int b = (int)blockIdx.x / A.a.n_kv;
   it.g = (int)blockIdx.x - b * A.a.n_kv;
-  const int chunk = paged_cut<ROWS * 2>(A, part).many;
+  const PagedSeq first = lane_seq(A, threadIdx.x & 63);
+  const int chunk = paged_cut(A, first).many;
   auto tiles = [&](const PagedSeq& q) { return (q.T * A.a.G + ROWS - 1) / ROWS; };
   Found f;
-  if (!find_entry<ROWS * 2>(A, b, [&](const PagedSeq& q) {
-        const bool mine = q.T > 0 && !paged_few(A, q);
-        return make_uint2(mine ? (uint32_t)(tiles(q) * paged_chunks(q.n, chunk)) : 0u, 0u);
+  if (!find_entry(A, first, b, [&](const PagedSeq& q) {
+        return make_uint2(paged_few(A, q) ? 0u : (uint32_t)(tiles(q) * paged_chunks(q.n, chunk)), 0u);
       }, f))
     return false;
-  const PagedSeq q = paged_seq(A, f.s);
+  const PagedSeq q = f.q;
   const int n_chunks = paged_chunks(q.n, chunk), back = f.within / n_chunks, c = f.within - back * n_chunks;
   it.tok0 = q.tok0;
   it.T = q.T;
@@ -75,6 +68,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
   it.j0 = c * chunk;
   it.j1 = n_chunks == 1 || q.n - it.j0 < chunk ? q.n : it.j0 + chunk;
   it.slot = n_chunks > 1 ? (int)blockIdx.x : -1;
+  it.n_chunks = n_chunks;
   it.table = A.table + (int64_t)f.s * A.table_stride;
   return true;
 }
@@ -367,8 +361,10 @@ void attn_kernel(const Args A) {
   if (!row_ok) return;
   const float l = l_run + __shfl_xor(l_run, 32);
   if constexpr (PAGED) {
+    const int row = wave * 32 + l32;
+    if (A.notes && h == 0 && it.j0 == 0)
+      A.notes[(int64_t)(it.tok0 + t) * a.H + head] = row_note(it.slot, it.n_chunks, row, true);
     if (it.slot >= 0) {
-      const int row = wave * 32 + l32;
       float* orow = partial_o(A.part_many, it.slot, ROWS, D) + row * D;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)

@@ -7,6 +7,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "ckv_internal.h"
 #include "ckv_plan.h"
 
@@ -81,6 +83,8 @@ int check_cache(const ckv_attn_desc* d, const ckv_paged_cache* c) {
 int check_batch(const ckv_attn_desc* d, const ckv_paged_batch* b) {
   if (!b || b->num_seqs < 1 || b->total_q < 0 || b->max_q < 0 || b->max_kv < 0) return CKV_ERR_INVALID_ARG;
   if (b->num_seqs > CKV_MAX_PAGED_SEQS) return CKV_ERR_UNSUPPORTED;
+  // positions of the tiles that are requested ahead, in 32 bits
+  if (b->max_kv > CKV_MAX_PAGED_KV) return CKV_ERR_UNSUPPORTED;
   // rows of a KV head, counted in 32 bits
   if ((int64_t)b->total_q * (d->num_q_heads / d->num_kv_heads) >= ((int64_t)1 << 30)) return CKV_ERR_UNSUPPORTED;
   return CKV_OK;
@@ -92,17 +96,36 @@ int32_t few_target(const ckv_attn_desc* d) {
 }
 constexpr int32_t kManyTarget = ckv::kCUs;  // and of the tile kernel
 
-// Bytes of the partial results that the kernel for few rows may leave (at most
-// two rounds of slots are split, see paged_share), and the tile kernel (one).
-size_t few_bytes(const ckv_attn_desc* d, const ckv_paged_batch* b) {
-  const int64_t rows = (int64_t)b->max_q * (d->num_q_heads / d->num_kv_heads);
-  if (b->max_kv <= ckv::kFewLeast) return 0;
-  return (size_t)2 * few_target(d) * (rows < ckv::kFewRows ? rows : ckv::kFewRows) * (d->head_dim + 2) * sizeof(float);
+// Prompts of up to this many tiles of kAttnRows rows, over all KV heads, take tiles of
+// kFewRows with the keys shared out to the waves: large tiles would leave CUs empty, small
+// ones read K and V again for every 32 rows. Large against small, in us:
+//   head dim 64:  bf16 64 tiles 45 / 21, 256 tiles 86 / 80, 376 tiles 127 / 154;
+//                 fp32 64 tiles 281 / 77, 256 tiles 562 / 367
+//   head dim 128: bf16 64 tiles 25 / 17, 128 tiles 42 / 39, 192 tiles 55 / 62;
+//                 fp32 128 tiles 261 / 152, 192 tiles 372 / 279, but four prompts of
+//                 160 tiles in all 85 / 113
+int64_t prefill_few_tiles(const ckv_attn_desc* d) {
+  return d->head_dim == 64 ? ckv::kCUs : d->dtype == CKV_F32 ? ckv::kCUs * 3 / 4 : ckv::kCUs / 2;
 }
-size_t many_bytes(const ckv_attn_desc* d, const ckv_paged_batch* b) {
+
+// What a batch of these bounds needs of the workspace: partial results of requests
+// of few rows (slots for twice kFewRounds rounds, as a split request has two chunks
+// at least) and of the tile kernel (one round), and a note per row.
+struct PagedSpace {
+  int32_t few_slots;
+  size_t few, many, notes;  // bytes
+};
+PagedSpace paged_space(const ckv_attn_desc* d, const ckv_paged_batch* b) {
   const int64_t rows = (int64_t)b->max_q * (d->num_q_heads / d->num_kv_heads);
-  if (rows <= ckv::kFewRows || b->max_kv <= ckv::kManyLeast) return 0;
-  return (size_t)kManyTarget * ckv::kAttnRows * (d->head_dim + 2) * sizeof(float);
+  const size_t row = (size_t)(d->head_dim + 2) * sizeof(float);
+  PagedSpace s = {};
+  if (b->max_kv > ckv::kFewLeast) {
+    s.few_slots = 2 * ckv::kFewRounds * few_target(d);
+    s.few = s.few_slots * std::min<int64_t>(rows, ckv::kFewRows) * row;
+    s.notes = (size_t)b->total_q * d->num_q_heads * sizeof(ckv::RowNote);
+  }
+  if (rows > ckv::kFewRows && b->max_kv > ckv::kManyLeast) s.many = (size_t)kManyTarget * ckv::kAttnRows * row;
+  return s;
 }
 
 // Whether [a, a + n) and [b, b + m) (numbers of int32) share an element.
@@ -138,13 +161,43 @@ int ckv_prefill_attention(const ckv_attn_desc* desc, const ckv_packed_attn* a,
   p.a.kv_sh = a->kv_stride_head * eb;
   for (int32_t i0 = 0; i0 < num_seqs; i0 += ckv::kPrefillSeqs) {
     p.n = num_seqs - i0 < ckv::kPrefillSeqs ? num_seqs - i0 : ckv::kPrefillSeqs;
-    p.tile[0] = 0;
-    for (int32_t i = 0; i <= p.n; ++i) {
-      p.tok[i] = cu_seqlens[i0 + i];
-      if (i > 0) p.tile[i] = p.tile[i - 1] + (int32_t)ceil_div((p.tok[i] - p.tok[i - 1]) * G, ckv::kAttnRows);
+    const int32_t* cu = cu_seqlens + i0;
+    const int32_t n = p.n;
+    auto len = [&](int32_t i) { return cu[i + 1] - cu[i]; };
+    int32_t longest = 0;
+    int64_t tiles = 0;
+    for (int32_t i = 0; i < n; ++i) {
+      longest = std::max(longest, len(i));
+      tiles += ceil_div(len(i) * G, ckv::kAttnRows);
     }
-    const hipError_t e = ckv::launch_prefill(desc->dtype, desc->head_dim, p, p.tile[p.n] * desc->num_kv_heads,
-                                             (hipStream_t)stream);
+    const bool few = tiles * desc->num_kv_heads <= prefill_few_tiles(desc);
+    const int64_t rows_per = few ? ckv::kFewRows : ckv::kAttnRows;
+    // A tile's work is its last row's position. Tiles run from long to short, in
+    // bands of position over all prompts, so that no long one starts when the others
+    // end: seven prompts of 1 to 4013 tokens
+    // took 220 us one after the other and take 210 so.
+    const int32_t bands = n == 1 ? 1 : std::min(ckv::kPrefillSeqs / n, 16);
+    p.n = 0;
+    p.tile[0] = 0;
+    for (int32_t b = bands - 1; b >= 0; --b) {
+      auto below = [&](int32_t i, int32_t band) {  // prompt i's tiles in the bands under this one
+        const int64_t rows = std::min((int64_t)longest * band / bands, (int64_t)len(i)) * G;
+        return (int32_t)(rows == len(i) * G ? ceil_div(rows, rows_per) : rows / rows_per);
+      };
+      for (int32_t i = 0; i < n; ++i) {
+        const int32_t lo = below(i, b), hi = below(i, b + 1);
+        if (hi == lo) continue;
+        p.tok[p.n] = cu[i];
+        p.len[p.n] = len(i);
+        p.top[p.n] = hi - 1;
+        p.tile[p.n + 1] = p.tile[p.n] + hi - lo;
+        ++p.n;
+      }
+    }
+    if (p.n == 0) continue;  // no token
+    const int grid = p.tile[p.n] * desc->num_kv_heads;
+    const hipError_t e = few ? ckv::launch_prefill_few(desc->dtype, desc->head_dim, p, grid, (hipStream_t)stream)
+                             : ckv::launch_prefill(desc->dtype, desc->head_dim, p, grid, (hipStream_t)stream);
     if (e != hipSuccess) return status(e);
   }
   return CKV_OK;
@@ -216,7 +269,8 @@ int ckv_paged_write(const ckv_attn_desc* desc, const ckv_paged_cache* cache, con
 
 size_t ckv_paged_workspace_bytes(const ckv_attn_desc* desc, const ckv_paged_batch* batch) {
   if (check_desc(desc) != CKV_OK || check_batch(desc, batch) != CKV_OK) return 0;
-  return few_bytes(desc, batch) + many_bytes(desc, batch) + 256;
+  const PagedSpace s = paged_space(desc, batch);
+  return s.few + s.many + s.notes + 256;
 }
 
 int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
@@ -255,7 +309,10 @@ int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
   p.page_size = cache->page_size;
   p.div = ckv::page_div(cache->page_size);
   p.part = static_cast<float*>(workspace);
-  p.part_many = reinterpret_cast<float*>(static_cast<char*>(workspace) + few_bytes(desc, batch));
+  const PagedSpace space = paged_space(desc, batch);
+  p.part_many = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.few);
+  p.notes = space.notes ? reinterpret_cast<ckv::RowNote*>(static_cast<char*>(workspace) + space.few + space.many) : nullptr;
+  p.few_slots = space.few_slots;
   // Requests of few and of many rows have a kernel each; one request with many
   // takes the latter whatever its rows turn out to be
   const int64_t N = batch->num_seqs, n_kv = desc->num_kv_heads, G = desc->num_q_heads / n_kv;
@@ -266,7 +323,6 @@ int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
   p.many_target = kManyTarget;
   const hipStream_t st = (hipStream_t)stream;
   hipError_t e = hipSuccess;
-  int64_t merge = 0;
   if (p.has_many) {
     // row tiles: whole ones of all rows, and one more each for what is left
     int64_t tiles = batch->total_q * G / ckv::kAttnRows + N;
@@ -275,22 +331,15 @@ int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
     if (split > p.many_target) split = p.many_target;
     const int64_t grid = split > tiles * n_kv ? split : tiles * n_kv;
     if ((e = ckv::launch_paged_many(desc->dtype, desc->head_dim, p, (int)grid, st)) != hipSuccess) return status(e);
-    if (batch->max_kv > ckv::kManyLeast)  // at least two slots per split tile
-      merge += p.many_target / 2 * ckv::kAttnRows / ckv::paged_merge_rows(desc->head_dim);
   }
   if (p.few_rows > 0) {
-    int64_t grid = N * n_kv + p.few_target;
+    int64_t grid = N * n_kv + ckv::kFewRounds * p.few_target;
     if (N * n_kv * ceil_div(batch->max_kv, ckv::kFewLeast) < grid)
       grid = N * n_kv * ceil_div(batch->max_kv, ckv::kFewLeast);
     if (grid < N * n_kv) grid = N * n_kv;
     if ((e = ckv::launch_paged_few(desc->dtype, desc->head_dim, p, (int)grid, st)) != hipSuccess) return status(e);
-    if (batch->max_kv > ckv::kFewLeast) {
-      // at least two of the slots per split request and KV head
-      const int64_t by_slots = (int64_t)p.few_target * p.few_rows, by_rows = (int64_t)batch->total_q * desc->num_q_heads;
-      merge += by_slots < by_rows ? by_slots : by_rows;
-    }
   }
-  return status(ckv::launch_paged_merge(desc->dtype, desc->head_dim, p, (int)merge, st));
+  return p.notes ? status(ckv::launch_paged_merge(desc->dtype, desc->head_dim, p, st)) : CKV_OK;
 }
 
 }  // extern "C"

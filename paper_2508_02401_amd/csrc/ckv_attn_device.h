@@ -111,6 +111,28 @@ __device__ __forceinline__ int clamp_int(int x, int lo, int hi) {
   return x < lo ? lo : (x > hi ? hi : x);
 }
 
+// ---- packed prompts ----
+// Block b of the grid: KV head b % n_kv (neighbouring blocks go to different
+// XCDs, so with 8 KV heads each XCD's L2 holds one head's K and V), row tiles in
+// the launch's order, a range of a prompt's tiles from its last on.
+struct PromptTile {
+  int tok0, T, g, rt;
+};
+__device__ __forceinline__ PromptTile prompt_tile(const PrefillArgs& A) {
+  PromptTile p;
+  const int b = (int)blockIdx.x / A.a.n_kv;
+  p.g = (int)blockIdx.x - b * A.a.n_kv;
+  int lo = 0, hi = A.n;  // the last range whose first tile is at most b
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (A.tile[mid] <= b) lo = mid; else hi = mid;
+  }
+  p.tok0 = A.tok[lo];
+  p.T = A.len[lo];
+  p.rt = A.top[lo] - (b - A.tile[lo]);
+  return p;
+}
+
 // ---- paged batches -----------------------------------------------------------
 __device__ __forceinline__ int page_at(const PageDiv& d, int x) {
   return (int)(((uint64_t)(uint32_t)x * d.mul) >> d.shift);
@@ -137,101 +159,125 @@ __device__ __forceinline__ int paged_chunks(int n, int chunk) {
   return n <= chunk ? 1 : (n + chunk - 1) / chunk;
 }
 
-// Sum over the workgroup, for every thread of it.
-template <int NT>
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* part) {
+// What follows is worked out by every wave for itself, 64 requests at a time, one
+// per lane, with no barrier: for 64 requests and fewer they are read once and stay
+// in registers. With sums and searches over the whole workgroup a step of four
+// drafted requests took 24 us in place of 16.
+__device__ __forceinline__ PagedSeq lane_seq(const PagedArgs& A, int s) {
+  PagedSeq q = {};
+  if (s < A.num_seqs) q = paged_seq(A, s);
+  return q;
+}
+// f(request) for this lane's requests.
+template <class F>
+__device__ __forceinline__ void each_seq(const PagedArgs& A, const PagedSeq& first, F f) {
+  f(first);
+  for (int s = 64 + (threadIdx.x & 63); s < A.num_seqs; s += 64) f(paged_seq(A, s));
+}
+template <int K>
+__device__ __forceinline__ void wave_sums(int64_t (&x)[K]) {
 #pragma unroll
-  for (int i = 32; i > 0; i >>= 1) x += __shfl_xor(x, i);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
-  __syncthreads();
-  int64_t sum = 0;
+  for (int i = 32; i > 0; i >>= 1)
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) sum += part[i];
-  __syncthreads();
-  return sum;
+    for (int k = 0; k < K; ++k) x[k] += __shfl_xor(x[k], i);
 }
 
 // Keys per workgroup. Every workgroup of the batch's launches works this out for
 // itself from the requests' lengths (the host knows bounds only). `work` is the
 // sum of the keys over the `base` items (row tiles times KV heads) of a launch,
-// `target` its workgroups in one round. An even share of work / target keys would
-// leave up to one short workgroup per item over, in a second round; with
-// work / (target - base) all fit into one. Past half a round of items the share
-// would grow to more than twice the even one, and the even one stays. Shares are
-// whole tiles of 64 keys and at least `least`.
-constexpr int kUnsplit = 0x7FFFFFC0;
-__device__ __forceinline__ int paged_share(int64_t work, int64_t base, int target, int least, bool split) {
-  if (!split && 2 * base > target) return kUnsplit;
-  const int64_t parts = 2 * base <= target ? target - base : target;
-  const int64_t c = ((work + parts - 1) / parts + 63) / 64 * 64;
-  return (int)(c < least ? least : c > kUnsplit ? kUnsplit : c);
+// `target` its workgroups in one round. Up to half a round of items, all workgroups
+// are to fit into one round: an even share of work / target keys does where the
+// lengths divide well; otherwise it leaves up to one short workgroup per item
+// over, and the share is work / (target - base), with which they always fit. Past
+// half a round of items, the kernel for few rows takes small shares, of which
+// the short requests' and the long ones' add up evenly; the tile kernel does not
+// split. Shares are whole UNITs and at least LEAST.
+constexpr int kUnsplit = 0x7FFFFF80;
+template <int LEAST, int UNIT>
+__device__ __forceinline__ int paged_share(int64_t work, int64_t parts) {
+  const double c = ceil((double)work / (double)parts * (1.0 / UNIT)) * UNIT;  // exact below 2^53
+  return c < LEAST ? LEAST : c > kUnsplit ? kUnsplit : (int)c;
+}
+
+// A 32-key tile for each of the four waves, and a tile of the tile kernel.
+__device__ __forceinline__ int few_share(int64_t work, int64_t parts) {
+  return paged_share<kFewLeast, 32 * kWaves>(work, parts);
+}
+__device__ __forceinline__ int many_share(int64_t work, int64_t parts) {
+  return paged_share<kManyLeast, 64>(work, parts);
 }
 
 struct PagedCut {
   int few, many;  // keys per workgroup of the two kernels
 };
-template <int NT>
-__device__ __forceinline__ PagedCut paged_cut(const PagedArgs& A, int64_t* part) {
-  int64_t few = 0, few_n = 0, many = 0, many_n = 0;
-  for (int s = threadIdx.x; s < A.num_seqs; s += NT) {
-    const PagedSeq q = paged_seq(A, s);
-    if (q.T == 0) continue;
-    if (paged_few(A, q)) {
-      few += q.n;
-      few_n += 1;
-    } else {
-      const int tiles = (q.T * A.a.G + kAttnRows - 1) / kAttnRows;
-      many += (int64_t)tiles * q.n;
-      many_n += tiles;
-    }
+__device__ __forceinline__ PagedCut paged_cut(const PagedArgs& A, const PagedSeq& first) {
+  int64_t x[4] = {};  // keys and items of the two
+  auto tiles = [&](const PagedSeq& q) { return (q.T * A.a.G + kAttnRows - 1) / kAttnRows; };
+  each_seq(A, first, [&](const PagedSeq& q) {
+    const bool few = paged_few(A, q);
+    const int n = q.T == 0 ? 0 : few ? 1 : tiles(q);
+    x[0] += few ? (int64_t)n * q.n : 0;
+    x[1] += few ? n : 0;
+    x[2] += few ? 0 : (int64_t)n * q.n;
+    x[3] += few ? 0 : n;
+  });
+  wave_sums(x);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] *= A.a.n_kv;
+  const bool few_fits = 2 * x[1] <= A.few_target, many_fits = 2 * x[3] <= A.many_target;
+  PagedCut c;
+  c.few = few_share(x[0], few_fits ? A.few_target : (int64_t)A.few_target * kFewRounds);
+  c.many = many_fits ? many_share(x[2], A.many_target) : kUnsplit;
+  if (few_fits || many_fits) {  // workgroups with the even shares
+    int64_t y[2] = {};
+    each_seq(A, first, [&](const PagedSeq& q) {
+      const bool few = paged_few(A, q);
+      const int n = q.T == 0 ? 0 : paged_chunks(q.n, few ? c.few : c.many);
+      y[0] += few ? n : 0;
+      y[1] += few ? 0 : (int64_t)tiles(q) * n;
+    });
+    wave_sums(y);
+    if (few_fits && y[0] * A.a.n_kv > A.few_target) c.few = few_share(x[0], A.few_target - x[1]);
+    if (many_fits && y[1] * A.a.n_kv > A.many_target) c.many = many_share(x[2], A.many_target - x[3]);
   }
-  PagedCut c = {};
-  if (A.few_rows > 0) {
-    // at most 4096 requests and 2^43 keys: both fit one number
-    const int64_t f = block_sum<NT>(few * 8192 + few_n, part);
-    c.few = paged_share((f >> 13) * A.a.n_kv, (f & 8191) * A.a.n_kv, A.few_target, kFewLeast, true);
-  }
-  if (A.has_many) {
-    const int64_t m = block_sum<NT>(many, part), n = block_sum<NT>(many_n, part);
-    c.many = paged_share(m * A.a.n_kv, n * A.a.n_kv, A.many_target, kManyLeast, false);
-  }
+  c.few = __builtin_amdgcn_readfirstlane(c.few);  // the same in every lane: in scalar registers from here on
+  c.many = __builtin_amdgcn_readfirstlane(c.many);
   return c;
 }
 
 // The request that entry b of a list of requests' entries belongs to, with
-// count(s, q) entries (x) each; and a second number (y) summed over the
-// requests before it.
+// count(q) entries (x) each; and a second number (y) summed over the requests
+// before it.
 struct Found {
-  int s, within;      // request, entry within it
+  PagedSeq q;         // the request
+  int s, within;      // its number, entry within it
   uint32_t before;    // sum of y
 };
-template <int NT, class Count>
-__device__ __forceinline__ bool find_entry(const PagedArgs& A, int b, Count count, Found& f) {
-  __shared__ uint32_t wsum[NT / 64];
-  __shared__ int res[3];
-  if (threadIdx.x == 0) res[0] = -1;
+template <class Count>
+__device__ __forceinline__ bool find_entry(const PagedArgs& A, const PagedSeq& first, int b, Count count, Found& f) {
+  const int lane = threadIdx.x & 63;
   uint32_t x0 = 0, y0 = 0;
-  for (int s0 = 0; s0 < A.num_seqs; s0 += NT) {
-    const int s = s0 + (int)threadIdx.x;
+  for (int s0 = 0; s0 < A.num_seqs; s0 += 64) {
+    const PagedSeq q = s0 == 0 ? first : lane_seq(A, s0 + lane);
     uint2 c = make_uint2(0u, 0u);
-    if (s < A.num_seqs) c = count(paged_seq(A, s));
-    uint32_t x_all, y_all;
-    const uint32_t x = x0 + block_excl_scan<NT>(c.x, wsum, x_all);
-    const uint32_t y = y0 + block_excl_scan<NT>(c.y, wsum, y_all);
-    if ((uint32_t)b >= x && (uint32_t)b - x < c.x) {
-      res[0] = s;
-      res[1] = (int)((uint32_t)b - x);
-      res[2] = (int)y;
+    if (q.T > 0) c = count(q);
+    const uint32_t x = x0 + wave_incl_scan(c.x), y = y0 + wave_incl_scan(c.y);
+    const uint64_t hit = __ballot((uint32_t)b < x && (uint32_t)b >= x - c.x);
+    if (hit) {
+      const int l = __ffsll((unsigned long long)hit) - 1;
+      auto of = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+      f.q.tok0 = of(q.tok0);
+      f.q.T = of(q.T);
+      f.q.n = of(q.n);
+      f.s = s0 + l;
+      f.within = of((int)((uint32_t)b - (x - c.x)));
+      f.before = (uint32_t)of((int)(y - c.y));
+      return true;
     }
-    __syncthreads();
-    if (res[0] >= 0) break;
-    x0 += x_all;
-    y0 += y_all;
+    x0 = (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+    y0 = (uint32_t)__builtin_amdgcn_readlane((int)y, 63);
   }
-  f.s = __builtin_amdgcn_readfirstlane(res[0]);
-  f.within = __builtin_amdgcn_readfirstlane(res[1]);
-  f.before = (uint32_t)__builtin_amdgcn_readfirstlane(res[2]);
-  return f.s >= 0;
+  return false;
 }
 
 // The factor of a partial result (maximum, sum) towards the maximum m: 0 for
@@ -247,6 +293,15 @@ __device__ __forceinline__ float* partial_o(float* part, int64_t slot, int rows,
 }
 __device__ __forceinline__ float2* partial_ml(float* part, int64_t slot, int rows, int D) {
   return reinterpret_cast<float2*>(part + slot * rows * (D + 2) + rows * D);
+}
+
+__device__ __forceinline__ RowNote row_note(int64_t slot, int n_chunks, int row, bool many) {
+  RowNote x = {};
+  if (slot >= 0) {
+    x.where = (uint32_t)slot | (many ? 0x80000000u : 0u);
+    x.what = (uint32_t)n_chunks | (uint32_t)row << 16;
+  }
+  return x;
 }
 
 // A row's log-sum-exp from its running maximum (in exp2 units) and sum.

@@ -305,16 +305,30 @@ struct AttnArgs {
 
 constexpr int kAttnRows = 256;  // query rows of a KV head per workgroup
 
-// Packed prompts: prompt i's rows are tok[i] .. tok[i + 1], its row tiles (per
-// KV head) tile[i] .. tile[i + 1].
+// Packed prompts as ranges of their row tiles (per KV head), in the order in which
+// they run: range i is of the prompt with len[i] tokens from row tok[i] on, its
+// tiles top[i], top[i] - 1, .. are the launch's tile[i] .. tile[i + 1].
 constexpr int kPrefillSeqs = CKV_PREFILL_SEQS;
 struct PrefillArgs {
   AttnArgs a;
   int32_t n;
-  int32_t tok[kPrefillSeqs + 1];
+  int32_t tok[kPrefillSeqs];
+  int32_t len[kPrefillSeqs];
+  int32_t top[kPrefillSeqs];
   int32_t tile[kPrefillSeqs + 1];
 };
 static_assert(sizeof(PrefillArgs) <= 4096, "prompts travel as kernel arguments");
+
+// How a row of a paged batch was split, for the join: slot of its first chunk (of the
+// tile kernel's slots, or those for few rows), chunks (0 if not split), and its
+// place in a slot. 16 bits hold the chunks: slots are at most a few thousand.
+struct RowNote {
+  uint32_t where, what;
+  __host__ __device__ bool many() const { return where >> 31; }
+  __host__ __device__ int slot() const { return (int)(where & 0x7FFFFFFF); }
+  __host__ __device__ int n() const { return (int)(what & 0xFFFF); }
+  __host__ __device__ int row() const { return (int)(what >> 16); }
+};
 
 struct PagedArgs {
   AttnArgs a;
@@ -333,10 +347,16 @@ struct PagedArgs {
   int32_t few_rows;           // requests of up to this many rows per KV head go to the few kernel
   int32_t has_many;           // the tile kernel is launched
   int32_t few_target, many_target;  // workgroups in one round
+  int32_t few_slots;          // slots for requests of few rows
+  RowNote* notes;             // [total_q][H], null where no keys can be split
 };
 constexpr int kFewRows = 32;     // rows per KV head of the kernel for few
 constexpr int kFewLeast = 128;   // keys per workgroup, at least
 constexpr int kManyLeast = 1024;
+// Rounds of shares where there are many requests: 64 requests of 64 to 8192 tokens, 8 KV
+// heads, take 97 / 90 / 95 us with 2 / 3 / 4 (small shares end together, but each costs
+// its own start)
+constexpr int kFewRounds = 3;
 
 struct PageWriteArgs {
   const char* k;
@@ -358,12 +378,11 @@ struct PagePlanArgs {
 };
 
 hipError_t launch_prefill(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st);
+hipError_t launch_prefill_few(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st);
 hipError_t launch_paged_many(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
 hipError_t launch_paged_few(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
-// Joins what the two left in parts: a workgroup per row of the few kernel's split
-// requests, one per paged_merge_rows(d) rows of the tile kernel's.
-hipError_t launch_paged_merge(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st);
-inline int paged_merge_rows(int d) { return 1024 / d; }
+// Joins what the two left in parts.
+hipError_t launch_paged_merge(int dtype, int d, const PagedArgs& p, hipStream_t st);
 hipError_t launch_page_write(const PageWriteArgs& w, hipStream_t st);
 hipError_t launch_page_plan(const PagePlanArgs& p, hipStream_t st);
 

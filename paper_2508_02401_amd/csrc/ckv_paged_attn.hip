@@ -1,13 +1,14 @@
-// gfx950 (MI355X) attention of few new tokens per request over a paged cache
-// (decoding steps), and the join of what is split along the keys.
+// gfx950 (MI355X) attention of 32 query rows per workgroup: few new tokens per
+// request over a paged cache (decoding steps), and prompts too small to fill the
+// chip with larger tiles; and the join of what is split along the keys.
 //
-// paged_few_kernel: up to 32 query rows (a KV head's G heads x T tokens), a
-//   workgroup per (request, KV head, chunk of its keys). A cache row is read
-//   once, so the bound is the stream, and what counts is how much of it is in
-//   flight: every wave owns 32-key tiles, whose K and V go from memory straight
-//   into the wave's part of LDS, the next tile's K requested as soon as this
-//   one's is in registers (the same for V), with no barrier between waves. The
-//   waves' results meet in LDS.
+// few_kernel: up to 32 query rows (of a KV head's G heads x T tokens), a
+//   workgroup per (request, KV head, chunk of its keys) or per (prompt, KV head,
+//   row tile). The keys go round the waves, which need no barrier between them:
+//   every wave owns 32-key tiles, whose K and V go from memory straight into the
+//   wave's part of LDS, the next tile's K requested as soon as this one's is in
+//   registers (the same for V). The waves' results meet in LDS. Over a cache each
+//   row is read once, so the bound is the stream; a prompt's come from L2.
 // paged_merge_kernel: the chunks' partial results (of this kernel and of the tile
 //   kernel) rescaled to the common maximum and added in order.
 #include <math.h>
@@ -19,9 +20,58 @@ namespace {
 
 using namespace dev;
 
-template <int DT, int D>
+// A workgroup's part: rows row0 .. of the T * G of a request whose last T of n keys
+// are its query tokens from row tok0 on; keys j0 .. j1.
+struct FewItem {
+  int tok0, T, n, g, row0, j0, j1;
+  int64_t slot;           // where its partial result goes, -1 where the keys are not split
+  int n_chunks;
+  const int32_t* table;   // paged: the request's block table
+};
+
+__device__ __forceinline__ bool find_few(const PagedArgs& A, FewItem& it) {
+  const int b = (int)blockIdx.x / A.a.n_kv;
+  it.g = (int)blockIdx.x - b * A.a.n_kv;
+  const PagedSeq first = lane_seq(A, threadIdx.x & 63);
+  const int chunk = paged_cut(A, first).few;
+  Found f;
+  if (!find_entry(A, first, b, [&](const PagedSeq& q) {
+        const uint32_t n = paged_few(A, q) ? paged_chunks(q.n, chunk) : 0;
+        return make_uint2(n, n > 1 ? n : 0);
+      }, f))
+    return false;
+  const PagedSeq q = f.q;
+  const int n_chunks = paged_chunks(q.n, chunk);
+  it.tok0 = q.tok0;
+  it.T = q.T;
+  it.n = q.n;
+  it.row0 = 0;
+  it.j0 = f.within * chunk;
+  it.j1 = n_chunks == 1 || q.n - it.j0 < chunk ? q.n : it.j0 + chunk;
+  it.slot = n_chunks > 1 ? (int64_t)f.before * A.a.n_kv + (int64_t)it.g * n_chunks + f.within : -1;
+  it.n_chunks = n_chunks;
+  it.table = A.table + (int64_t)f.s * A.table_stride;
+  return true;
+}
+
+__device__ __forceinline__ bool find_few(const PrefillArgs& A, FewItem& it) {
+  const PromptTile p = prompt_tile(A);
+  it.tok0 = p.tok0;
+  it.T = it.n = p.T;
+  it.g = p.g;
+  it.row0 = p.rt * kFewRows;
+  const int last = it.row0 + kFewRows < p.T * A.a.G ? it.row0 + kFewRows - 1 : p.T * A.a.G - 1;
+  it.j0 = 0;
+  it.j1 = last / A.a.G + 1;
+  it.slot = -1;
+  it.n_chunks = 1;
+  it.table = nullptr;
+  return true;
+}
+
+template <int DT, int D, bool PAGED, class Args>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(DT == 2 ? 1 : 2)))
-void paged_few_kernel(const PagedArgs A) {
+void few_kernel(const Args A) {
   constexpr int EB = Elt<DT>::bytes;
   constexpr int ROWB = D * EB;       // bytes per cache row
   constexpr int NV = ROWB / 16;      // 16-byte chunks per row: 8, 16 or 32
@@ -35,64 +85,65 @@ void paged_few_kernel(const PagedArgs A) {
   __shared__ uint4 kl[kWaves][VEC];  // chunk c of row t at position c ^ swz(t), V's at c ^ vswz(t)
   __shared__ uint4 vl[kWaves][VEC];
   __shared__ float2 ml[kWaves][32];
-  __shared__ int64_t sums[kWaves];
   const AttnArgs& a = A.a;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = (int)blockIdx.x / a.n_kv, g = (int)blockIdx.x - b * a.n_kv;
-  const int chunk = paged_cut<kThreads>(A, sums).few;
-  Found f;
-  if (!find_entry<kThreads>(A, b, [&](const PagedSeq& q) {
-        const uint32_t n = q.T > 0 && paged_few(A, q) ? paged_chunks(q.n, chunk) : 0;
-        return make_uint2(n, n > 1 ? n : 0);
-      }, f))
-    return;
-  const PagedSeq sq = paged_seq(A, f.s);
-  const int n_chunks = paged_chunks(sq.n, chunk);
-  const int32_t* table = A.table + (int64_t)f.s * A.table_stride;
-  const int G = a.G, R = sq.T * G;
-  const int j0 = f.within * chunk;
-  const int j1 = n_chunks == 1 || sq.n - j0 < chunk ? sq.n : j0 + chunk;
+  FewItem it;
+  if (!find_few(A, it)) return;
+  const int G = a.G, g = it.g, j0 = it.j0, j1 = it.j1;
+  const int R = it.T * G - it.row0 < kFewRows ? it.T * G - it.row0 : kFewRows;  // rows of this workgroup
   const int nt = (j1 - j0 + KT - 1) / KT;
   const char* kbase = a.k + (int64_t)g * a.kv_sh;
   const char* vbase = a.v + (int64_t)g * a.kv_sh;
+  if constexpr (!PAGED) {
+    kbase += (int64_t)it.tok0 * a.kv_st;
+    vbase += (int64_t)it.tok0 * a.kv_st;
+  }
   const float alpha = a.alpha;
 
   auto swz = [](int t) { return ROWB >= 256 ? (t & 15) : ((t >> 1) & 7); };
   // V rows of fp32 are read along their columns, which meets every bank as it is
   auto vswz = [&](int t) { return DT == 2 ? 0 : swz(t); };
   const int lrow = lane / NV, lpos = lane % NV;
-  // the page of key l32 of tile tl, -1 for keys that are not there
+  // the page of key l32 of tile tl (0 where there are no pages), -1 for keys that are not there
   auto page_of = [&](int tl) {
     const int key = j0 + tl * KT + l32;
     int id = -1;
     if (key < j1) {
-      const int p = page_at(A.div, key);
-      if (p < A.table_width) id = to_global(table)[p];
-      if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
+      if constexpr (PAGED) {
+        const int p = page_at(A.div, key);
+        if (p < A.table_width) id = to_global(it.table)[p];
+        if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
+      } else {
+        id = 0;
+      }
     }
     return id;
   };
-  // tile tl of base: non-temporal, each cache row is read once. Keys that are not
-  // there read a row of page 0.
+  // tile tl of base; a cache's rows, read once, are non-temporal. Keys that are not
+  // there read some valid row.
   auto fetch = [&](const char* base, int tl, int page, uint4* slot, auto swizzle) {
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
       const int t = i * RPL + lrow, key = j0 + tl * KT + t;
-      const int id = __shfl(page, t);
-      const int64_t off = (int64_t)(id < 0 ? 0 : id) * A.kv_sp +
-                          (int64_t)(key - page_at(A.div, key) * A.page_size) * a.kv_st;
-      __builtin_amdgcn_global_load_lds(
-          reinterpret_cast<const uint4*>(base + off + (lpos ^ swizzle(t)) * 16), slot + i * 64, 16, 0, 2);
+      int64_t off;
+      if constexpr (PAGED) {
+        const int id = __shfl(page, t);
+        off = (int64_t)(id < 0 ? 0 : id) * A.kv_sp + (int64_t)(key - page_at(A.div, key) * A.page_size) * a.kv_st;
+      } else {
+        off = (int64_t)(key < j1 ? key : j1 - 1) * a.kv_st;
+      }
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(base + off + (lpos ^ swizzle(t)) * 16),
+                                       slot + i * 64, 16, 0, PAGED ? 2 : 0);
     }
   };
   // query row r = token * G + head; lane half h holds chunks 2c + h of it
-  const int r = l32 < R ? l32 : R - 1;
-  const int t = r / G, limit = sq.n - sq.T + t;
+  const int r = it.row0 + (l32 < R ? l32 : R - 1);
+  const int t = r / G, limit = it.n - it.T + t;
   uint4 q[NC];
   {
     const CKV_GLOBAL u32x4* src =
-        (const CKV_GLOBAL u32x4*)(to_global(a.q) + (int64_t)(sq.tok0 + t) * a.q_st +
+        (const CKV_GLOBAL u32x4*)(to_global(a.q) + (int64_t)(it.tok0 + t) * a.q_st +
                                   (int64_t)(g * G + r - t * G) * a.q_sh) + h;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -269,7 +320,6 @@ void paged_few_kernel(const PagedArgs A) {
           make_float4(o[nb][4 * v4], o[nb][4 * v4 + 1], o[nb][4 * v4 + 2], o[nb][4 * v4 + 3]);
     }
   __syncthreads();
-  const int64_t slot = (int64_t)f.before * a.n_kv + (int64_t)g * n_chunks + f.within;
   for (int e = tid; e < R * (D / 4); e += kThreads) {
     const int rr = e / (D / 4), c = e - rr * (D / 4);
     float m = ml[0][rr].x;
@@ -289,151 +339,168 @@ void paged_few_kernel(const PagedArgs A) {
       acc.z += y.z * fct;
       acc.w += y.w * fct;
     }
-    if (n_chunks > 1) {
-      *reinterpret_cast<float4*>(partial_o(A.part, slot, A.few_rows, D) + rr * D + 4 * c) = acc;
-      if (c == 0) partial_ml(A.part, slot, A.few_rows, D)[rr] = make_float2(m - kBias, ls);
-    } else {
-      const int tt = rr / G, head = g * G + rr - tt * G;
-      const float inv = row_scale(ls);
-      store4<DT>(a.out + (int64_t)(sq.tok0 + tt) * a.o_st + (int64_t)head * a.o_sh + 4 * c * EB,
-                 acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      if (c == 0 && a.lse) a.lse[(int64_t)head * a.lse_sh + sq.tok0 + tt] = row_lse(m - kBias, ls);
+    const int tt = (it.row0 + rr) / G, head = g * G + it.row0 + rr - tt * G;
+    if constexpr (PAGED) {
+      if (A.notes && c == 0 && j0 == 0)
+        A.notes[(int64_t)(it.tok0 + tt) * a.H + head] = row_note(it.slot, it.n_chunks, rr, false);
+      if (it.slot >= 0) {
+        *reinterpret_cast<float4*>(partial_o(A.part, it.slot, A.few_rows, D) + rr * D + 4 * c) = acc;
+        if (c == 0) partial_ml(A.part, it.slot, A.few_rows, D)[rr] = make_float2(m - kBias, ls);
+        continue;
+      }
     }
+    const float inv = row_scale(ls);
+    store4<DT>(a.out + (int64_t)(it.tok0 + tt) * a.o_st + (int64_t)head * a.o_sh + 4 * c * EB,
+               acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (c == 0 && a.lse) a.lse[(int64_t)head * a.lse_sh + it.tok0 + tt] = row_lse(m - kBias, ls);
   }
 }
 
-// One row of a request of few rows (all thread groups of D / 4 lanes share its
-// chunks), or a thread group per row of the others.
+// Joins the partial results of the rows whose keys were split, which the two kernels
+// noted per row. A workgroup takes a row with all its thread groups of D / 4 lanes,
+// or, where there are many rows, a row per thread group unless they have many chunks.
+// Bound by the latency of its three dependent reads: 6 us for 32 rows in 128 parts, 8 us
+// for 2048 rows of 512 parts in all; with every workgroup working the cuts out
+// again in place of reading the notes it took 8 and 12 us.
+__host__ __device__ inline int merge_rows_per(const PagedArgs& A, int groups) {
+  return (int64_t)A.total_q * A.a.H <= 16 * kCUs ? 1 : groups;
+}
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A) {
   constexpr int C4 = D / 4, NG = kThreads / C4, U = 8;
   constexpr int EB = Elt<DT>::bytes;
   __shared__ float4 acc_l[NG][C4];
   __shared__ float2 ml_l[NG];
-  __shared__ int64_t sums[kWaves];
   const AttnArgs& a = A.a;
   const int grp = threadIdx.x / C4, c = threadIdx.x % C4;
-  const PagedCut cut = paged_cut<kThreads>(A, sums);
-  // entries are this launch's workgroups; y counts the slots per KV head of the two
-  // kernels, few in the low half (at most 2 * few_target), many in the high half
-  // (at most many_target, where any are split)
-  Found f;
-  if (!find_entry<kThreads>(A, (int)blockIdx.x, [&](const PagedSeq& q) {
-        if (q.T == 0) return make_uint2(0u, 0u);
-        const bool few = paged_few(A, q);
-        const uint32_t n = (uint32_t)paged_chunks(q.n, few ? cut.few : cut.many), R = q.T * a.G;
-        if (few) return n < 2 ? make_uint2(0u, 0u) : make_uint2(R * a.n_kv, n);
-        if (cut.many == kUnsplit) return make_uint2(0u, 0u);
-        return make_uint2(n < 2 ? 0u : (R + NG - 1) / NG * a.n_kv, ((R + kAttnRows - 1) / kAttnRows * n) << 16);
-      }, f))
-    return;
-  const PagedSeq q = paged_seq(A, f.s);
-  const bool few = paged_few(A, q);
-  const int R = q.T * a.G, n = paged_chunks(q.n, few ? cut.few : cut.many);
-  int r, g;
-  int64_t slot0;     // of the row's first chunk
-  int step;          // slots between chunks
-  const float* part;
-  int rows;
-  if (few) {
-    g = f.within / R;
-    r = f.within - g * R;
-    slot0 = (int64_t)(f.before & 0xFFFF) * a.n_kv + (int64_t)g * n;
-    step = 1;
-    part = A.part;
-    rows = A.few_rows;
-  } else {
-    // split requests' items are the blocks of the tile kernel's launch, in the
-    // order in which find_item numbers them
-    const int per = (R + NG - 1) / NG;
-    g = f.within / per;
-    r = (f.within - g * per) * NG + grp;
-    if (r >= R) r = R - 1;
-    const int tiles = (R + kAttnRows - 1) / kAttnRows, back = tiles - 1 - r / kAttnRows;
-    slot0 = (int64_t)((f.before >> 16) + back * n) * a.n_kv + g;
-    step = a.n_kv;
-    part = A.part_many;
-    rows = kAttnRows;
-  }
-  const int row = few ? r : r % kAttnRows;
-  const int64_t words = (int64_t)rows * (D + 2);
-  const int first = few ? grp : 0, stride = few ? NG : 1;
-  float m = -INFINITY, l = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = first; i0 < n; i0 += U * stride) {
-    float2 x[U];
-    float4 y[U];
+  const int rows_per = merge_rows_per(A, NG);
+  const int64_t lo = (int64_t)clamp_int(to_global(A.cu_q)[0], 0, A.total_q) * a.H;
+  const int64_t hi = (int64_t)clamp_int(to_global(A.cu_q)[A.num_seqs], 0, A.total_q) * a.H;
+  // Row's note, one without chunks where it has none. The notes of rows that no
+  // request covers may hold anything: what they name stays inside the workspace.
+  auto note_of = [&](int64_t row) {
+    RowNote x = {};
+    if (row >= lo && row < hi) x = A.notes[row];
+    const int cap = x.many() ? A.many_target : A.few_slots, step = x.many() ? a.n_kv : 1;
+    const bool ok = x.n() >= 2 && (int64_t)x.slot() + (int64_t)(x.n() - 1) * step < cap &&
+                    x.row() < (x.many() ? kAttnRows : A.few_rows);
+    return ok ? x : RowNote{};
+  };
+  // chunks first, first + stride, .. of a row
+  auto gather = [&](const RowNote x, int first, int stride, float& m, float& l, float4& acc) {
+    const int rows = x.many() ? kAttnRows : A.few_rows, step = x.many() ? a.n_kv : 1, n = x.n(), row = x.row();
+    const int64_t words = (int64_t)rows * (D + 2);
+    const float* part = (x.many() ? A.part_many : A.part) + x.slot() * words;
+    m = -INFINITY;
+    l = 0.f;
+    acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i0 = first; i0 < n; i0 += U * stride) {
+      float2 x[U];
+      float4 y[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * stride;
-      const float* p = part + (slot0 + (int64_t)(i < n ? i : first) * step) * words;
-      x[u] = reinterpret_cast<const float2*>(p + rows * D)[row];
-      y[u] = reinterpret_cast<const float4*>(p + row * D)[c];
-      if (i >= n) x[u] = make_float2(-INFINITY, 0.f);
-    }
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * stride;
+        const float* p = part + (int64_t)(i < n ? i : first) * step * words;
+        x[u] = reinterpret_cast<const float2*>(p + rows * D)[row];
+        y[u] = reinterpret_cast<const float4*>(p + row * D)[c];
+        if (i >= n) x[u] = make_float2(-INFINITY, 0.f);
+      }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float m_new = fmaxf(m, x[u].x);
-      const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(x[u], m_new);
-      m = m_new;
-      l = l * old + x[u].y * f_new;
-      acc.x = acc.x * old + (f_new == 0.f ? 0.f : y[u].x * f_new);
-      acc.y = acc.y * old + (f_new == 0.f ? 0.f : y[u].y * f_new);
-      acc.z = acc.z * old + (f_new == 0.f ? 0.f : y[u].z * f_new);
-      acc.w = acc.w * old + (f_new == 0.f ? 0.f : y[u].w * f_new);
+      for (int u = 0; u < U; ++u) {
+        const float m_new = fmaxf(m, x[u].x);
+        const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(x[u], m_new);
+        m = m_new;
+        l = l * old + x[u].y * f_new;
+        acc.x = acc.x * old + (f_new == 0.f ? 0.f : y[u].x * f_new);
+        acc.y = acc.y * old + (f_new == 0.f ? 0.f : y[u].y * f_new);
+        acc.z = acc.z * old + (f_new == 0.f ? 0.f : y[u].z * f_new);
+        acc.w = acc.w * old + (f_new == 0.f ? 0.f : y[u].w * f_new);
+      }
     }
-  }
-  if (few) {
+  };
+  auto put = [&](int64_t row, float m, float l, float4 acc) {
+    const int tok = (int)(row / a.H), head = (int)(row - (int64_t)tok * a.H);
+    const float inv = row_scale(l);
+    store4<DT>(a.out + (int64_t)tok * a.o_st + (int64_t)head * a.o_sh + 4 * c * EB, acc.x * inv, acc.y * inv,
+               acc.z * inv, acc.w * inv);
+    if (c == 0 && a.lse) a.lse[(int64_t)head * a.lse_sh + tok] = row_lse(m, l);
+  };
+  auto together = [&](int64_t row, const RowNote x) {  // for the whole workgroup
+    if (x.n() < 2) return;
+    float m, l;
+    float4 acc;
+    gather(x, grp, NG, m, l, acc);
     acc_l[grp][c] = acc;
     if (c == 0) ml_l[grp] = make_float2(m, l);
     __syncthreads();
-    if (grp > 0) return;
-    for (int i = 1; i < NG; ++i) {
-      const float2 x = ml_l[i];
-      const float4 y = acc_l[i][c];
-      const float m_new = fmaxf(m, x.x);
-      const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(x, m_new);
-      m = m_new;
-      l = l * old + x.y * f_new;
-      acc.x = acc.x * old + y.x * f_new;
-      acc.y = acc.y * old + y.y * f_new;
-      acc.z = acc.z * old + y.z * f_new;
-      acc.w = acc.w * old + y.w * f_new;
+    if (grp == 0) {
+      for (int i = 1; i < NG; ++i) {
+        const float2 z = ml_l[i];
+        const float4 y = acc_l[i][c];
+        const float m_new = fmaxf(m, z.x);
+        const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(z, m_new);
+        m = m_new;
+        l = l * old + z.y * f_new;
+        acc.x = acc.x * old + y.x * f_new;
+        acc.y = acc.y * old + y.y * f_new;
+        acc.z = acc.z * old + y.z * f_new;
+        acc.w = acc.w * old + y.w * f_new;
+      }
+      put(row, m, l, acc);
+    }
+    __syncthreads();
+  };
+  for (int64_t row0 = (int64_t)blockIdx.x * rows_per; row0 < hi; row0 += (int64_t)gridDim.x * rows_per) {
+    if (rows_per == 1) {
+      together(row0, note_of(row0));
+      continue;
+    }
+    const RowNote mine = note_of(row0 + grp);
+    if (__syncthreads_or(mine.n() > 8 * U)) {
+      for (int i = 0; i < NG; ++i) together(row0 + i, note_of(row0 + i));
+    } else if (mine.n() >= 2) {
+      float m, l;
+      float4 acc;
+      gather(mine, 0, 1, m, l, acc);
+      put(row0 + grp, m, l, acc);
     }
   }
-  const int t = r / a.G, head = g * a.G + r - t * a.G;
-  const float inv = row_scale(l);
-  store4<DT>(a.out + (int64_t)(q.tok0 + t) * a.o_st + (int64_t)head * a.o_sh + 4 * c * EB, acc.x * inv,
-             acc.y * inv, acc.z * inv, acc.w * inv);
-  if (c == 0 && a.lse) a.lse[(int64_t)head * a.lse_sh + q.tok0 + t] = row_lse(m, l);
+}
+
+template <int D>
+hipError_t launch_merge(int dtype, const PagedArgs& p, hipStream_t st) {
+  constexpr int NG = kThreads / (D / 4);
+  const int64_t rows = (int64_t)p.total_q * p.a.H, per = merge_rows_per(p, NG), most = 64 * kCUs;
+  const int grid = (int)((rows + per - 1) / per < most ? (rows + per - 1) / per : most);
+  auto kernel = dtype == CKV_BF16 ? paged_merge_kernel<0, D> : dtype == CKV_F16 ? paged_merge_kernel<1, D> : paged_merge_kernel<2, D>;
+  return launch(kernel, grid, kThreads, st, Timing(), p);
+}
+
+template <bool PAGED, class Args>
+hipError_t launch_few(int dtype, int d, const Args& p, int grid, hipStream_t st) {
+  if (grid == 0) return hipSuccess;
+  const Timing none;
+  if (d == 128) {
+    if (dtype == CKV_BF16) return launch(few_kernel<0, 128, PAGED, Args>, grid, kThreads, st, none, p);
+    if (dtype == CKV_F16) return launch(few_kernel<1, 128, PAGED, Args>, grid, kThreads, st, none, p);
+    return launch(few_kernel<2, 128, PAGED, Args>, grid, kThreads, st, none, p);
+  }
+  if (dtype == CKV_BF16) return launch(few_kernel<0, 64, PAGED, Args>, grid, kThreads, st, none, p);
+  if (dtype == CKV_F16) return launch(few_kernel<1, 64, PAGED, Args>, grid, kThreads, st, none, p);
+  return launch(few_kernel<2, 64, PAGED, Args>, grid, kThreads, st, none, p);
 }
 
 }  // namespace
 
 hipError_t launch_paged_few(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st) {
-  if (grid == 0) return hipSuccess;
-  const Timing none;
-  if (d == 128) {
-    if (dtype == CKV_BF16) return launch(paged_few_kernel<0, 128>, grid, kThreads, st, none, p);
-    if (dtype == CKV_F16) return launch(paged_few_kernel<1, 128>, grid, kThreads, st, none, p);
-    return launch(paged_few_kernel<2, 128>, grid, kThreads, st, none, p);
-  }
-  if (dtype == CKV_BF16) return launch(paged_few_kernel<0, 64>, grid, kThreads, st, none, p);
-  if (dtype == CKV_F16) return launch(paged_few_kernel<1, 64>, grid, kThreads, st, none, p);
-  return launch(paged_few_kernel<2, 64>, grid, kThreads, st, none, p);
+  return launch_few<true>(dtype, d, p, grid, st);
+}
+hipError_t launch_prefill_few(int dtype, int d, const PrefillArgs& p, int grid, hipStream_t st) {
+  return launch_few<false>(dtype, d, p, grid, st);
 }
 
-hipError_t launch_paged_merge(int dtype, int d, const PagedArgs& p, int grid, hipStream_t st) {
-  if (grid == 0) return hipSuccess;
-  const Timing none;
-  if (d == 128) {
-    if (dtype == CKV_BF16) return launch(paged_merge_kernel<0, 128>, grid, kThreads, st, none, p);
-    if (dtype == CKV_F16) return launch(paged_merge_kernel<1, 128>, grid, kThreads, st, none, p);
-    return launch(paged_merge_kernel<2, 128>, grid, kThreads, st, none, p);
-  }
-  if (dtype == CKV_BF16) return launch(paged_merge_kernel<0, 64>, grid, kThreads, st, none, p);
-  if (dtype == CKV_F16) return launch(paged_merge_kernel<1, 64>, grid, kThreads, st, none, p);
-  return launch(paged_merge_kernel<2, 64>, grid, kThreads, st, none, p);
+hipError_t launch_paged_merge(int dtype, int d, const PagedArgs& p, hipStream_t st) {
+  return d == 128 ? launch_merge<128>(dtype, p, st) : launch_merge<64>(dtype, p, st);
 }
 
 }  // namespace ckv
