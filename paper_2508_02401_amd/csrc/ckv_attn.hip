@@ -10,6 +10,15 @@
 // lanes; the running maximum and sum of the softmax; O^T += V^T P^T with MFMA,
 // whose P operand is the lane's own logits in place. V is transposed on the
 // way out of LDS (ds_read_b64_tr_b16).
+//
+// What bounds it: a wave and tile of 64 keys (bf16, d 128) take 1024 cycles of the
+// matrix units and about 950 of the vector units (528 of them the 32 exponentials),
+// and the two waves of a SIMD hardly overlap the one with the other: 4400
+// cycles per tile of 256 rows. 32768 tokens of 32 heads over 8 take 8.2 ms,
+// 1.07 PFLOP/s, where a library product of 8192^3 reaches 1.22. Running the second
+// four waves half a step behind the first, so that one half multiplies while
+// the other works out its weights, took 9.0 ms; alternating the two chains of
+// QK^T made no difference.
 #include <math.h>
 
 #include <type_traits>
@@ -118,8 +127,11 @@ void attn_kernel(const Args A) {
   const int nt = keys > it.j0 ? (keys + KT - 1) / KT : tl0;
 
   auto swz = [](int row) { return ROWB >= 256 ? (row & 15) : ((row >> 1) & 7); };
-  // V rows of fp32 are read along their columns, which meets every bank as it is
-  auto vswz = [&](int row) { return DT == 2 ? 0 : swz(row); };
+  // V of 16-bit types is read 4 keys of 64 bytes at a time, which meet every bank once if
+  // they lie in different quarters of the 256 bytes (with K's swizzle, 59% of the LDS
+  // cycles were bank conflicts and a prompt of 32768 tokens took 8.6 ms, not 8.2);
+  // rows of fp32 are read along their columns, which does as it is
+  auto vswz = [&](int row) { return DT == 2 ? 0 : ROWB >= 256 ? (row & 3) * 4 : (row & 2) * 2; };
   const int lrow = lane / NV, lpos = lane % NV;
   const char* kbase = a.k + (int64_t)it.g * a.kv_sh;
   const char* vbase = a.v + (int64_t)it.g * a.kv_sh;
@@ -146,8 +158,8 @@ void attn_kernel(const Args A) {
     const int left = it.n - tl * KT;
     return left >= KT ? kAll : (1ull << left) - 1;
   };
-  // Requests tile tl. Keys that are not there read some valid row.
-  auto fetch = [&](int tl, int page, uint4* ks, uint4* vs) {
+  // Requests a tile's rows of K or V. Keys that are not there read some valid row.
+  auto fetch_one = [&](const char* base, int tl, int page, uint4* dst, auto swizzle) {
 #pragma unroll
     for (int i = 0; i < PT; ++i) {
       const int row = (i * NW + wave) * RPL + lrow;  // of the tile
@@ -162,11 +174,23 @@ void attn_kernel(const Args A) {
         const int key = tl * KT + row < it.n ? tl * KT + row : it.n - 1;
         off = (int64_t)key * a.kv_st;
       }
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(kbase + off + (lpos ^ swz(row)) * 16),
-                                       ks + (i * NW + wave) * 64, 16, 0, 0);
-      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(vbase + off + (lpos ^ vswz(row)) * 16),
-                                       vs + (i * NW + wave) * 64, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const uint4*>(base + off + (lpos ^ swizzle(row)) * 16),
+                                       dst + (i * NW + wave) * 64, 16, 0, 0);
     }
+  };
+  auto fetch = [&](int tl, int page, uint4* ks, uint4* vs) {
+    fetch_one(kbase, tl, page, ks, swz);
+    fetch_one(vbase, tl, page, vs, vswz);
+  };
+  // Keys that are not there count as zeros in V: for the rows that this wave requested.
+  auto clear_v = [&](uint64_t seen, uint4* vs) {
+    if (seen == kAll) return;
+#pragma unroll
+    for (int i = 0; i < PT; ++i) {
+      const int row = (i * NW + wave) * RPL + lrow;
+      if (!((seen >> row) & 1)) vs[(i * NW + wave) * 64 + lane] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    wait_vm<0>();
   };
 
   // lane half h holds chunks 2c + h of its query row
@@ -204,6 +228,78 @@ void attn_kernel(const Args A) {
 
   f32x16 o[NB];
   float m_run, l_run;
+  // S^T = K Q^T of a tile
+  auto logits = [&](const uint4* ks, f32x16 (&s)[KB]) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      __builtin_amdgcn_sched_barrier(0);
+      s[kb] = f32x16{};
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        s[kb] = mfma_chunk<DT>(ks[(kb * 32 + l32) * NV + ((2 * c + h) ^ swz(l32))], q[c], s[kb]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // logits to weights, with the keys `sees` (if `hides`), and the running maximum and sum
+  auto weights = [&](f32x16 (&s)[KB], bool hides, uint64_t sees) {
+    if (hides) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const uint32_t bits = (uint32_t)(sees >> (32 * kb)) >> (4 * h);
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!(bits & (1u << acc_row(v, 0)))) s[kb][v] = -INFINITY;
+      }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * alpha;
+    if (__any(mx > m_run + kSlack)) {
+      const float m_new = fmaxf(m_run, mx);
+      const float resc = m_run == -INFINITY ? 0.f : weight_exp2<DT>(m_run - m_new);
+      l_run *= resc;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) o[nb] *= resc;
+      m_run = m_new;
+    }
+    const float ms = m_run == -INFINITY ? 0.f : m_run - kBias;
+    float psum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        s[kb][v] = weight_exp2<DT>(fmaf(s[kb][v], alpha, -ms));
+        psum += s[kb][v];
+      }
+    l_run += psum;
+  };
+  // the keys of tile tl, of which `vis` are there, that this lane's row sees, one bit each
+  auto seen_keys = [&](int tl, uint64_t vis, bool& hides) {
+    const int rel = limit - tl * KT;
+    hides = vis != kAll || tl * KT + KT - 1 > lim_lo;
+    uint64_t sees = vis;
+    if (hides && rel < KT - 1) sees &= rel < 0 ? 0 : (2ull << rel) - 1;
+    return sees;
+  };
+  // P^T operands: MFMA step km takes this lane's keys acc_row(8km .. 8km+7, h)
+  // = 16km + 4h + (0..3) and 16km + 8 + 4h + (0..3), in that order
+  auto p_chunk = [&](const f32x16 (&s)[KB], int km) {
+    float p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = s[km >> 1][8 * (km & 1) + i];
+    return round_chunk<DT>(p);
+  };
+  auto not_finite = [&]() {
+    float bad = 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) bad = fmaf(o[nb][v], 0.f, bad);
+    return active && bad != 0.f;
+  };
   // A row's hidden keys have weight 0, but 0 times a value that is not finite
   // is not 0. If an output came out not finite, the tiles are taken again, first
   // without such values, then for what every row sees of them.
@@ -221,14 +317,7 @@ void attn_kernel(const Args A) {
     page = page_of(tl0 + 1);
     auto step = [&](int tl, uint4* ks, uint4* vs, uint4* ks_next, uint4* vs_next) {
       wait_vm<0>();  // this wave's part of the tile
-      if (seen != kAll) {  // keys that are not there count as zeros in V
-#pragma unroll
-        for (int i = 0; i < PT; ++i) {
-          const int row = (i * NW + wave) * RPL + lrow;
-          if (!((seen >> row) & 1)) vs[(i * NW + wave) * 64 + lane] = make_uint4(0u, 0u, 0u, 0u);
-        }
-        wait_vm<0>();
-      }
+      clear_v(seen, vs);
       barrier();
       const uint64_t vis = seen;
       if (tl + 1 < nt) {
@@ -238,11 +327,8 @@ void attn_kernel(const Args A) {
       }
       const int j0 = tl * KT;
       if (!active || j0 > lim_hi) return;
-      // the keys of the tile that this lane's row sees, one bit each
-      const bool hides = vis != kAll || j0 + KT - 1 > lim_lo;
-      uint64_t sees = vis;
-      const int rel = limit - j0;
-      if (hides && rel < KT - 1) sees &= rel < 0 ? 0 : (2ull << rel) - 1;
+      bool hides;
+      const uint64_t sees = seen_keys(tl, vis, hides);
       const char* vt = reinterpret_cast<const char*>(vs);
       if constexpr (MODE == kLeftOut) {
 #pragma unroll
@@ -270,58 +356,13 @@ void attn_kernel(const Args A) {
         return;
       }
       f32x16 s[KB];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        __builtin_amdgcn_sched_barrier(0);
-        s[kb] = f32x16{};
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-          s[kb] = mfma_chunk<DT>(ks[(kb * 32 + l32) * NV + ((2 * c + h) ^ swz(l32))], q[c], s[kb]);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (hides) {
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-          const uint32_t bits = (uint32_t)(sees >> (32 * kb)) >> (4 * h);
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (!(bits & (1u << acc_row(v, 0)))) s[kb][v] = -INFINITY;
-        }
-      }
-      float mx = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32)) * alpha;
-      if (__any(mx > m_run + kSlack)) {
-        const float m_new = fmaxf(m_run, mx);
-        const float resc = m_run == -INFINITY ? 0.f : weight_exp2<DT>(m_run - m_new);
-        l_run *= resc;
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb) o[nb] *= resc;
-        m_run = m_new;
-      }
-      const float ms = m_run == -INFINITY ? 0.f : m_run - kBias;
-      float psum = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s[kb][v] = weight_exp2<DT>(fmaf(s[kb][v], alpha, -ms));
-          psum += s[kb][v];
-        }
-      l_run += psum;
+      logits(ks, s);
+      weights(s, hides, sees);
       if constexpr (DT != 2) {
-        // P^T operands: MFMA step km takes this lane's keys acc_row(8km .. 8km+7, h)
-        // = 16km + 4h + (0..3) and 16km + 8 + 4h + (0..3), in that order
 #pragma unroll
         for (int km = 0; km < KB * 2; ++km) {
           __builtin_amdgcn_sched_barrier(0);
-          float p[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = s[km >> 1][8 * (km & 1) + i];
-          const uint4 ph = round_chunk<DT>(p);
+          const uint4 ph = p_chunk(s, km);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
             uint4 x, va = v_chunk(vt, nb, km);
@@ -346,12 +387,7 @@ void attn_kernel(const Args A) {
       step(tl, k0, v0, k1, v1);
       if (tl + 1 < nt) step(tl + 1, k1, v1, k0, v0);
     }
-    float bad = 0.f;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) bad = fmaf(o[nb][v], 0.f, bad);
-    return active && bad != 0.f;
+    return not_finite();
   };
   if (__syncthreads_or(pass(std::integral_constant<Pass, kPlain>()))) {
     pass(std::integral_constant<Pass, kStripped>());

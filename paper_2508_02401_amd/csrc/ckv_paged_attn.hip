@@ -102,8 +102,10 @@ void few_kernel(const Args A) {
   const float alpha = a.alpha;
 
   auto swz = [](int t) { return ROWB >= 256 ? (t & 15) : ((t >> 1) & 7); };
-  // V rows of fp32 are read along their columns, which meets every bank as it is
-  auto vswz = [&](int t) { return DT == 2 ? 0 : swz(t); };
+  // V of 16-bit types is read 4 keys of 64 bytes at a time, which meet every bank once if
+  // they lie in different quarters of the 256 bytes; rows of fp32 are read along
+  // their columns, which does as it is
+  auto vswz = [&](int t) { return DT == 2 ? 0 : ROWB >= 256 ? (t & 3) * 4 : (t & 2) * 2; };
   const int lrow = lane / NV, lpos = lane % NV;
   // the page of key l32 of tile tl (0 where there are no pages), -1 for keys that are not there
   auto page_of = [&](int tl) {
