@@ -313,6 +313,7 @@ int ckv_paged_attention(const ckv_attn_desc* desc, const ckv_paged_cache* cache,
   p.part_many = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.few);
   p.notes = space.notes ? reinterpret_cast<ckv::RowNote*>(static_cast<char*>(workspace) + space.few + space.many) : nullptr;
   p.few_slots = space.few_slots;
+  p.many_slots = space.many ? kManyTarget : 0;
   // Requests of few and of many rows have a kernel each; one request with many
   // takes the latter whatever its rows turn out to be
   const int64_t N = batch->num_seqs, n_kv = desc->num_kv_heads, G = desc->num_q_heads / n_kv;

@@ -347,7 +347,7 @@ struct PagedArgs {
   int32_t few_rows;           // requests of up to this many rows per KV head go to the few kernel
   int32_t has_many;           // the tile kernel is launched
   int32_t few_target, many_target;  // workgroups in one round
-  int32_t few_slots;          // slots for requests of few rows
+  int32_t few_slots, many_slots;  // slots that the workspace has for the two
   RowNote* notes;             // [total_q][H], null where no keys can be split
 };
 constexpr int kFewRows = 32;     // rows per KV head of the kernel for few

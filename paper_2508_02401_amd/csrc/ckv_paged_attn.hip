@@ -383,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
   auto note_of = [&](int64_t row) {
     RowNote x = {};
     if (row >= lo && row < hi) x = A.notes[row];
-    const int cap = x.many() ? A.many_target : A.few_slots, step = x.many() ? a.n_kv : 1;
+    const int cap = x.many() ? A.many_slots : A.few_slots, step = x.many() ? a.n_kv : 1;
     const bool ok = x.n() >= 2 && (int64_t)x.slot() + (int64_t)(x.n() - 1) * step < cap &&
                     x.row() < (x.many() ? kAttnRows : A.few_rows);
     return ok ? x : RowNote{};

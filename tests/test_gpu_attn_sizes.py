@@ -133,3 +133,57 @@ def test_shares_follow_the_lengths_within_one_graph():
         at = _sums(st.add)
         o, _, tol, _ = attend(*st.rows(1))
         check(out[at[1]:at[2]], o, tol, "step %d" % i)
+
+
+def test_notes_of_rows_that_no_kernel_takes():
+    # more rows than the bounds say: nobody writes their notes, and what the workspace held there
+    # names parts of the large tiles' results, for which it has no room
+    H, n_kv, d = 8, 2, 64
+    st = Step(50, torch.bfloat16, H, n_kv, d, 16, [3000], [40])
+    desc = ckv.attn_desc(H, n_kv, d, torch.bfloat16)
+    ints = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    batch = ckv.paged_batch(ints([0, 40, 40]), ints([3040, 0]), ints(st.table * 2), 40, 1, 3040)
+    n = ckv.ckv_paged_workspace_bytes(desc, batch)
+    ws = torch.full((n // 8,), (2 << 32) + 0x80000000, dtype=torch.int64, device="cuda")
+    out = torch.full((40, H, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    ckv.ckv_paged_attention(desc, ckv.paged_cache(st.k, st.v), batch, st.q, out, ws)
+    torch.cuda.synchronize()
+    assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("add", [1, 60])
+def test_pages_past_32_bits(add):
+    # the request's pages lie behind the first 4 GiB of the pool, some before
+    H, n_kv, d, page, n = 8, 2, 64, 64, 700
+    gen = torch.Generator().manual_seed(add)
+    n_pages = (5 << 30) // (n_kv * page * d * 2)
+    pages = [n_pages - 1 - 3 * i if i % 3 else i for i in range(-(-n // page))]
+    rand = lambda *shape: torch.randn(shape, generator=gen).to(torch.bfloat16).cuda()  # noqa: E731
+    kp, vp = (torch.empty(n_pages, n_kv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v, q = rand(n_kv, n, d), rand(n_kv, n, d), rand(add, H, d)
+    ints = lambda xs: torch.tensor(xs, dtype=torch.int32, device="cuda")  # noqa: E731
+    desc, cache = ckv.attn_desc(H, n_kv, d), ckv.paged_cache(kp, vp)
+    ckv.ckv_paged_write(desc, cache, k, v, ints([pages[j // page] * page + j % page for j in range(n)]))
+    batch = ckv.paged_batch(ints([0, add]), ints([n]), ints([pages]), add, add, n)
+    ws = torch.empty(ckv.ckv_paged_workspace_bytes(desc, batch), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(H, add, device="cuda")
+    ckv.ckv_paged_attention(desc, cache, batch, q, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    o, z, ot, zt = attend(q, k, v, torch.arange(n)[None] <= torch.arange(add)[:, None] + n - add)
+    check(out, o, ot, "out")
+    check(lse, z, zt, "lse")
+
+
+@pytest.mark.parametrize("n,H", [(300, 2), (1100, 64)])
+def test_rows_past_32_bits(n, H):
+    # tokens of K and V so far apart that the last lies behind the first 4 GiB, on both sides
+    # of the choice of tiles
+    n_kv, d = H // 2, 64
+    gap = (5 << 30) // 2 // n // 8 * 8
+    q, k, v = _inputs(n, torch.bfloat16, H, n_kv, d, n)
+    wide = torch.empty(n * gap + n_kv * d, dtype=torch.bfloat16, device="cuda")
+    kw = wide.as_strided((n_kv, n, d), (d, gap, 1))
+    vw = torch.empty_like(wide).as_strided((n_kv, n, d), (d, gap, 1))
+    kw.copy_(k), vw.copy_(v)
+    out, lse = _run(q, kw, vw, [0, n], n_kv)
+    _check(q, k, v, [0, n], out, lse)
