@@ -57,11 +57,11 @@ __device__ __forceinline__ bool find_item(const PrefillArgs& A, Item& it) {
 
 template <int ROWS>
 __device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
-  static_assert(ROWS == kAttnRows, "tiles as paged_cut counts them");
+  static_assert(ROWS == kAttnRows, "tiles as many_share counts them");
   const int b = (int)blockIdx.x / A.a.n_kv;
   it.g = (int)blockIdx.x - b * A.a.n_kv;
   const PagedSeq first = lane_seq(A, threadIdx.x & 63);
-  const int chunk = paged_cut(A, first).many;
+  const int chunk = many_share(A, first);
   auto tiles = [&](const PagedSeq& q) { return (q.T * A.a.G + ROWS - 1) / ROWS; };
   Found f;
   if (!find_entry(A, first, b, [&](const PagedSeq& q) {

@@ -182,16 +182,14 @@ __device__ __forceinline__ void wave_sums(int64_t (&x)[K]) {
     for (int k = 0; k < K; ++k) x[k] += __shfl_xor(x[k], i);
 }
 
-// Keys per workgroup. Every workgroup of the batch's launches works this out for
-// itself from the requests' lengths (the host knows bounds only). `work` is the
-// sum of the keys over the `base` items (row tiles times KV heads) of a launch,
-// `target` its workgroups in one round. Up to half a round of items, all workgroups
-// are to fit into one round: an even share of work / target keys does where the
-// lengths divide well; otherwise it leaves up to one short workgroup per item
-// over, and the share is work / (target - base), with which they always fit. Past
-// half a round of items, the kernel for few rows takes small shares, of which
-// the short requests' and the long ones' add up evenly; the tile kernel does not
-// split. Shares are whole UNITs and at least LEAST.
+// Keys per workgroup of a kernel, its share. Every workgroup works it out for itself
+// from the requests' lengths (the host knows bounds only). `work` is the sum of the
+// keys over the `base` items (row tiles times KV heads) of the launch, `target` its
+// workgroups in one round. Up to half a round of items, all workgroups are to fit
+// into one round: an even share of work / target keys does where the lengths divide
+// well; otherwise it leaves up to one short workgroup per item over, and with
+// work / (target - base) they always fit.
+// Shares are whole UNITs and at least LEAST.
 constexpr int kUnsplit = 0x7FFFFF80;
 template <int LEAST, int UNIT>
 __device__ __forceinline__ int paged_share(int64_t work, int64_t parts) {
@@ -199,50 +197,70 @@ __device__ __forceinline__ int paged_share(int64_t work, int64_t parts) {
   return c < LEAST ? LEAST : c > kUnsplit ? kUnsplit : (int)c;
 }
 
-// A 32-key tile for each of the four waves, and a tile of the tile kernel.
-__device__ __forceinline__ int few_share(int64_t work, int64_t parts) {
-  return paged_share<kFewLeast, 32 * kWaves>(work, parts);
-}
-__device__ __forceinline__ int many_share(int64_t work, int64_t parts) {
-  return paged_share<kManyLeast, 64>(work, parts);
-}
-
-struct PagedCut {
-  int few, many;  // keys per workgroup of the two kernels
-};
-__device__ __forceinline__ PagedCut paged_cut(const PagedArgs& A, const PagedSeq& first) {
-  int64_t x[4] = {};  // keys and items of the two
-  auto tiles = [&](const PagedSeq& q) { return (q.T * A.a.G + kAttnRows - 1) / kAttnRows; };
+// The kernel for few rows: a 32-key tile for each of the four waves. Past half a round
+// of items it takes small shares, of which the short requests' and the long ones'
+// add up evenly.
+__device__ __forceinline__ int few_share(const PagedArgs& A, const PagedSeq& first) {
+  int64_t x[2] = {};  // keys and items
   each_seq(A, first, [&](const PagedSeq& q) {
-    const bool few = paged_few(A, q);
-    const int n = q.T == 0 ? 0 : few ? 1 : tiles(q);
-    x[0] += few ? (int64_t)n * q.n : 0;
-    x[1] += few ? n : 0;
-    x[2] += few ? 0 : (int64_t)n * q.n;
-    x[3] += few ? 0 : n;
+    const bool mine = q.T > 0 && paged_few(A, q);
+    x[0] += mine ? q.n : 0;
+    x[1] += mine ? 1 : 0;
   });
   wave_sums(x);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] *= A.a.n_kv;
-  const bool few_fits = 2 * x[1] <= A.few_target, many_fits = 2 * x[3] <= A.many_target;
-  PagedCut c;
-  c.few = few_share(x[0], few_fits ? A.few_target : (int64_t)A.few_target * kFewRounds);
-  c.many = many_fits ? many_share(x[2], A.many_target) : kUnsplit;
-  if (few_fits || many_fits) {  // workgroups with the even shares
-    int64_t y[2] = {};
-    each_seq(A, first, [&](const PagedSeq& q) {
-      const bool few = paged_few(A, q);
-      const int n = q.T == 0 ? 0 : paged_chunks(q.n, few ? c.few : c.many);
-      y[0] += few ? n : 0;
-      y[1] += few ? 0 : (int64_t)tiles(q) * n;
-    });
+  x[0] *= A.a.n_kv;
+  x[1] *= A.a.n_kv;
+  auto share = [&](int64_t parts) { return paged_share<kFewLeast, 32 * kWaves>(x[0], parts); };
+  const bool fits = 2 * x[1] <= A.few_target;
+  int c = share(fits ? A.few_target : (int64_t)A.few_target * kFewRounds);
+  if (fits) {
+    int64_t y[1] = {};  // workgroups with even shares
+    each_seq(A, first, [&](const PagedSeq& q) { y[0] += q.T > 0 && paged_few(A, q) ? paged_chunks(q.n, c) : 0; });
     wave_sums(y);
-    if (few_fits && y[0] * A.a.n_kv > A.few_target) c.few = few_share(x[0], A.few_target - x[1]);
-    if (many_fits && y[1] * A.a.n_kv > A.many_target) c.many = many_share(x[2], A.many_target - x[3]);
+    if (y[0] * A.a.n_kv > A.few_target) c = share(A.few_target - x[1]);
   }
-  c.few = __builtin_amdgcn_readfirstlane(c.few);  // the same in every lane: in scalar registers from here on
-  c.many = __builtin_amdgcn_readfirstlane(c.many);
-  return c;
+  return __builtin_amdgcn_readfirstlane(c);  // the same in every lane: in scalar registers from here on
+}
+
+// The tile kernel: it does not split past half a round of items. Where even shares do not
+// fit, the smallest of 64 shares up to work / (target - base) that does, one per lane (500,
+// 300 and 100 tokens over 8000 each: 302 us with that last share, 213 so; for few rows the
+// search costs more than it saves, 31 to 37 us for 16 single tokens).
+__device__ __forceinline__ int many_share(const PagedArgs& A, const PagedSeq& first) {
+  auto tiles = [&](int T) { return (T * A.a.G + kAttnRows - 1) / kAttnRows; };
+  int64_t x[2] = {};  // keys and items
+  each_seq(A, first, [&](const PagedSeq& q) {
+    const int n = q.T > 0 && !paged_few(A, q) ? tiles(q.T) : 0;
+    x[0] += (int64_t)n * q.n;
+    x[1] += n;
+  });
+  wave_sums(x);
+  x[0] *= A.a.n_kv;
+  x[1] *= A.a.n_kv;
+  if (2 * x[1] > A.many_target) return kUnsplit;
+  auto share = [&](int64_t parts) { return paged_share<kManyLeast, 64>(x[0], parts); };
+  int lo = share(A.many_target);
+  const int hi = share(A.many_target - x[1]);
+  const int lane = threadIdx.x & 63;
+  // lane 0 tries lo, lane 63 hi, with which all fit
+  const int64_t step = ((int64_t)(hi - lo) * lane / 63 + 63) / 64 * 64;
+  const int c = lo + step > hi ? hi : (int)(lo + step);
+  const float r = 1.f / (float)c;
+  int64_t count = 0;
+  for (int s0 = 0; s0 < A.num_seqs; s0 += 64) {
+    const PagedSeq q = s0 == 0 ? first : lane_seq(A, s0 + lane);
+    for (uint64_t m = __ballot(q.T > 0 && !paged_few(A, q)); m; m &= m - 1) {
+      const int l = __ffsll((unsigned long long)m) - 1;
+      const int n = __builtin_amdgcn_readlane(q.n, l), T = __builtin_amdgcn_readlane(q.T, l);
+      int e = (int)((float)n * r);  // n / c rounded up: at most a few hundred, so at most one off
+      e += (int64_t)e * c < n ? 1 : 0;
+      e += (int64_t)e * c < n ? 1 : 0;
+      e -= (int64_t)(e - 1) * c >= n ? 1 : 0;
+      count += (int64_t)tiles(T) * (n <= c ? 1 : e);
+    }
+  }
+  const uint64_t fits = __ballot(count * A.a.n_kv <= A.many_target) | 1ull << 63;
+  return __builtin_amdgcn_readlane(c, __ffsll((unsigned long long)fits) - 1);
 }
 
 // The request that entry b of a list of requests' entries belongs to, with

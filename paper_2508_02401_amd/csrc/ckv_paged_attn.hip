@@ -33,7 +33,7 @@ __device__ __forceinline__ bool find_few(const PagedArgs& A, FewItem& it) {
   const int b = (int)blockIdx.x / A.a.n_kv;
   it.g = (int)blockIdx.x - b * A.a.n_kv;
   const PagedSeq first = lane_seq(A, threadIdx.x & 63);
-  const int chunk = paged_cut(A, first).few;
+  const int chunk = few_share(A, first);
   Found f;
   if (!find_entry(A, first, b, [&](const PagedSeq& q) {
         const uint32_t n = paged_few(A, q) ? paged_chunks(q.n, chunk) : 0;
