@@ -388,7 +388,8 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
                     x.row() < (x.many() ? kAttnRows : A.few_rows);
     return ok ? x : RowNote{};
   };
-  // chunks first, first + stride, .. of a row
+  // chunks first, first + stride, .. of a row. One of factor 0 is multiplied all the same:
+  // what it holds that is not finite reaches the row.
   auto gather = [&](const RowNote x, int first, int stride, float& m, float& l, float4& acc) {
     const int rows = x.many() ? kAttnRows : A.few_rows, step = x.many() ? a.n_kv : 1, n = x.n(), row = x.row();
     const int64_t words = (int64_t)rows * (D + 2);
@@ -405,7 +406,10 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
         const float* p = part + (int64_t)(i < n ? i : first) * step * words;
         x[u] = reinterpret_cast<const float2*>(p + rows * D)[row];
         y[u] = reinterpret_cast<const float4*>(p + row * D)[c];
-        if (i >= n) x[u] = make_float2(-INFINITY, 0.f);
+        if (i >= n) {  // no such chunk
+          x[u] = make_float2(-INFINITY, 0.f);
+          y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -413,10 +417,10 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
         const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(x[u], m_new);
         m = m_new;
         l = l * old + x[u].y * f_new;
-        acc.x = acc.x * old + (f_new == 0.f ? 0.f : y[u].x * f_new);
-        acc.y = acc.y * old + (f_new == 0.f ? 0.f : y[u].y * f_new);
-        acc.z = acc.z * old + (f_new == 0.f ? 0.f : y[u].z * f_new);
-        acc.w = acc.w * old + (f_new == 0.f ? 0.f : y[u].w * f_new);
+        acc.x = acc.x * old + y[u].x * f_new;
+        acc.y = acc.y * old + y[u].y * f_new;
+        acc.z = acc.z * old + y[u].z * f_new;
+        acc.w = acc.w * old + y[u].w * f_new;
       }
     }
   };
