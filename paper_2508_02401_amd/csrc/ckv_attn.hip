@@ -75,7 +75,7 @@ __device__ __forceinline__ bool find_item(const PagedArgs& A, Item& it) {
   it.n = q.n;
   it.rt = tiles(q) - 1 - back;
   it.j0 = c * chunk;
-  it.j1 = n_chunks == 1 || q.n - it.j0 < chunk ? q.n : it.j0 + chunk;
+  it.j1 = paged_chunk_end(q.n, chunk, c);
   it.slot = n_chunks > 1 ? (int)blockIdx.x : -1;
   it.n_chunks = n_chunks;
   it.table = A.table + (int64_t)f.s * A.table_stride;
@@ -146,7 +146,7 @@ void attn_kernel(const Args A) {
       const int key = tl * KT + (lane & (KT - 1));
       if (key < it.j1) {
         const int p = page_at(A.div, key);
-        if (p < A.table_width) id = to_global(it.table)[p];
+        if ((uint32_t)p < (uint32_t)A.table_width) id = to_global(it.table)[p];
         if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
       }
     }

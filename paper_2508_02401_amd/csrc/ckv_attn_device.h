@@ -153,11 +153,6 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& A, int s) {
 __device__ __forceinline__ bool paged_few(const PagedArgs& A, const PagedSeq& q) {
   return q.T * A.a.G <= A.few_rows;
 }
-// Chunks that a request's keys are cut into (one where it has none: its rows
-// are written all the same).
-__device__ __forceinline__ int paged_chunks(int n, int chunk) {
-  return n <= chunk ? 1 : (n + chunk - 1) / chunk;
-}
 
 // What follows is worked out by every wave for itself, 64 requests at a time, one
 // per lane, with no barrier: for 64 requests and fewer they are read once and stay

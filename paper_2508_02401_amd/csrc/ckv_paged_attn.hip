@@ -47,7 +47,7 @@ __device__ __forceinline__ bool find_few(const PagedArgs& A, FewItem& it) {
   it.n = q.n;
   it.row0 = 0;
   it.j0 = f.within * chunk;
-  it.j1 = n_chunks == 1 || q.n - it.j0 < chunk ? q.n : it.j0 + chunk;
+  it.j1 = paged_chunk_end(q.n, chunk, f.within);
   it.slot = n_chunks > 1 ? (int64_t)f.before * A.a.n_kv + (int64_t)it.g * n_chunks + f.within : -1;
   it.n_chunks = n_chunks;
   it.table = A.table + (int64_t)f.s * A.table_stride;
@@ -114,7 +114,7 @@ void few_kernel(const Args A) {
     if (key < j1) {
       if constexpr (PAGED) {
         const int p = page_at(A.div, key);
-        if (p < A.table_width) id = to_global(it.table)[p];
+        if ((uint32_t)p < (uint32_t)A.table_width) id = to_global(it.table)[p];
         if ((uint32_t)id >= (uint32_t)A.n_pages) id = -1;
       } else {
         id = 0;

@@ -156,4 +156,13 @@ inline PageDiv page_div(int32_t size) {
   return PageDiv{(uint32_t)((num + size - 1) / size), 31 + s};
 }
 
+// Chunks of up to `chunk` keys that a request's n are cut into; one where it has none, as its
+// rows are written all the same. n reaches CKV_MAX_PAGED_KV: n + chunk would pass 2^31.
+constexpr int32_t paged_chunks(int32_t n, int32_t chunk) { return n <= chunk ? 1 : 1 + (n - 1) / chunk; }
+
+// Chunk c's keys end before this one.
+constexpr int32_t paged_chunk_end(int32_t n, int32_t chunk, int32_t c) {
+  return n - c * chunk < chunk ? n : (c + 1) * chunk;
+}
+
 }  // namespace ckv
