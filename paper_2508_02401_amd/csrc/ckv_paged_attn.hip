@@ -406,13 +406,10 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
         const float* p = part + (int64_t)(i < n ? i : first) * step * words;
         x[u] = reinterpret_cast<const float2*>(p + rows * D)[row];
         y[u] = reinterpret_cast<const float4*>(p + row * D)[c];
-        if (i >= n) {  // no such chunk
-          x[u] = make_float2(-INFINITY, 0.f);
-          y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (i0 + u * stride >= n) break;  // what was read past the last one does not count
         const float m_new = fmaxf(m, x[u].x);
         const float old = part_weight(make_float2(m, l), m_new), f_new = part_weight(x[u], m_new);
         m = m_new;
