@@ -630,9 +630,9 @@ def paged_cache(k: torch.Tensor, v: torch.Tensor) -> ckv_paged_cache:
     """One layer's paged cache, k and v [n_pages, n_kv, page_size, d] with the same strides (any
     but the last's: a [n_pages, page_size, n_kv, d] pool is passed transposed)."""
     if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or \
-            k.stride(3) != 1:
+            k.device != v.device or k.stride(3) != 1:
         raise ValueError("paged_cache: k and v must be [n_pages, n_kv, page_size, d] with equal "
-                         "strides and types, d contiguous")
+                         "strides and types on one device, d contiguous")
     c = ckv_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                         k.shape[0], k.shape[2])
     c.tensors = (k, v)  # kept alive, and looked at by the calls
