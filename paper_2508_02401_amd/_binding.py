@@ -639,8 +639,16 @@ def paged_cache(k: torch.Tensor, v: torch.Tensor) -> ckv_paged_cache:
     return c
 
 
+def _tensors(what: str, struct, maker: str):
+    """The tensors that a struct points to, which only the function that made it knows."""
+    try:
+        return struct.tensors
+    except AttributeError:
+        raise ValueError("%s: takes what %s() returns, with its tensors" % (what, maker)) from None
+
+
 def _cache_arg(what: str, desc: ckv_attn_desc, cache: ckv_paged_cache):
-    k, v = cache.tensors
+    k, v = _tensors(what, cache, "paged_cache")
     if k.shape[1] != desc.num_kv_heads:
         raise ValueError("%s: the cache must have the descriptor's KV heads" % what)
     _pair(what, desc, k, v, 4)
@@ -720,7 +728,7 @@ def ckv_paged_attention(desc: ckv_attn_desc, cache: ckv_paged_cache, batch: ckv_
     a = _rows_arg(what, desc, q, out, lse)
     if q.shape[0] < batch.total_q:
         raise ValueError("%s: fewer rows than total_q" % what)
-    dev = _on_device(what, q, out, ck, workspace, lse, *batch.tensors)
+    dev = _on_device(what, q, out, ck, workspace, lse, *_tensors(what, batch, "paged_batch"))
     _call_on(dev, load().ckv_paged_attention, what,
              (ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(a),
               workspace.data_ptr(), workspace.numel() * workspace.element_size()), stream)

@@ -13,3 +13,20 @@ def test_pools_on_two_devices():
     for k, v in ((_pool(), _pool("meta")), (_pool("meta"), _pool())):
         with pytest.raises(ValueError, match="device"):
             ckv.paged_cache(k, v)
+
+
+def test_structs_that_were_filled_by_hand():
+    # exported for the C interface; the calls cannot look at the tensors behind their pointers
+    desc, pool = ckv.attn_desc(4, 2, 64), _pool()
+    cache = ckv.paged_cache(pool, pool)
+    ints = torch.zeros(9, dtype=torch.int32)
+    batch = ckv.paged_batch(ints[:4], ints[:3], ints.view(3, 3), 9, 4, 9)
+    q, k = torch.zeros(9, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 9, 64, dtype=torch.bfloat16)
+    bare_cache = ckv.ckv_paged_cache.from_buffer_copy(cache)
+    bare_batch = ckv.ckv_paged_batch.from_buffer_copy(batch)
+    with pytest.raises(ValueError, match="paged_cache"):
+        ckv.ckv_paged_write(desc, bare_cache, k, k, ints)
+    with pytest.raises(ValueError, match="paged_cache"):
+        ckv.ckv_paged_attention(desc, bare_cache, batch, q, torch.empty_like(q), ints)
+    with pytest.raises(ValueError, match="paged_batch"):
+        ckv.ckv_paged_attention(desc, cache, bare_batch, q, torch.empty_like(q), ints)
