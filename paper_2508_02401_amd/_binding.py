@@ -569,6 +569,13 @@ def _call_on(dev: int, fn, what: str, args, stream) -> None:
         raise CkvError(status, what)
 
 
+def _fits(what: str, **numbers: int) -> None:
+    """ctypes keeps the low 32 bits of a number, whatever stands above them."""
+    for name, x in numbers.items():
+        if not -0x80000000 <= x < 0x80000000:
+            raise ValueError("%s: %s = %d does not fit 32 bits" % (what, name, x))
+
+
 def _int32(what: str, name: str, t: torch.Tensor, dim: int = 1) -> torch.Tensor:
     if t.dtype is not torch.int32 or t.dim() != dim or (t.stride(-1) != 1 and t.numel() > 1):
         raise ValueError("%s: %s must be int32 with %d axes, the last contiguous" % (what, name, dim))
@@ -617,8 +624,9 @@ def ckv_prefill_attention(desc: ckv_attn_desc, q: torch.Tensor, k: torch.Tensor,
     if k.shape[:2] != (desc.num_kv_heads, q.shape[0]):
         raise ValueError("%s: k and v must be [n_kv, N, d]" % what)
     n = len(cu_seqlens) - 1
-    if n < 1 or cu_seqlens[n] > q.shape[0]:
+    if n < 1 or max(cu_seqlens) > q.shape[0]:
         raise ValueError("%s: cu_seqlens must hold 2 or more row numbers, none past N" % what)
+    _fits(what, cu_seqlens=min(cu_seqlens))
     a.k, a.v = k.data_ptr(), v.data_ptr()
     a.kv_stride_head, a.kv_stride_tok = k.stride(0), k.stride(1)
     cu = (ctypes.c_int32 * (n + 1))(*cu_seqlens)
@@ -674,6 +682,7 @@ def ckv_paged_plan(cached: torch.Tensor, add: torch.Tensor, table: torch.Tensor,
     _int32(what, "table", table, 2)
     if table.shape[0] != n:
         raise ValueError("%s: table must be [%d, width]" % (what, n))
+    _fits(what, page_size=page_size)
     p = ckv_page_plan(cached.data_ptr(), add.data_ptr(), n, page_size, table.data_ptr(),
                       table.stride(0), table.shape[1], free_pages.shape[0], free_pages.data_ptr(),
                       _ptr(free_head), cu_q.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
@@ -709,6 +718,7 @@ def paged_batch(cu_q: torch.Tensor, kv_len: torch.Tensor, table: torch.Tensor, t
     _int32(what, "cu_q", cu_q), _int32(what, "kv_len", kv_len), _int32(what, "table", table, 2)
     if cu_q.shape[0] != n + 1 or table.shape[0] != n:
         raise ValueError("paged_batch: cu_q must be [n + 1] and table [n, width] for kv_len [n]")
+    _fits(what, total_q=total_q, max_q=max_q, max_kv=max_kv)
     b = ckv_paged_batch(cu_q.data_ptr(), kv_len.data_ptr(), table.data_ptr(), table.stride(0),
                         table.shape[1], n, total_q, max_q, max_kv, 0)
     b.tensors = (cu_q, kv_len, table)

@@ -30,3 +30,19 @@ def test_structs_that_were_filled_by_hand():
         ckv.ckv_paged_attention(desc, bare_cache, batch, q, torch.empty_like(q), ints)
     with pytest.raises(ValueError, match="paged_batch"):
         ckv.ckv_paged_attention(desc, cache, bare_batch, q, torch.empty_like(q), ints)
+
+
+@pytest.mark.parametrize("over", [1 << 32, -(1 << 32), (1 << 32) * 3])
+def test_numbers_past_32_bits(over):
+    # their low 32 bits alone would be taken for other, valid ones
+    desc = ckv.attn_desc(4, 2, 64)
+    ints = torch.zeros(9, dtype=torch.int32)
+    for bad in ((9 + over, 4, 9), (9, 4 + over, 9), (9, 4, 9 + over)):
+        with pytest.raises(ValueError, match="32 bits"):
+            ckv.paged_batch(ints[:4], ints[:3], ints.view(3, 3), *bad)
+    one = ints[:1]
+    with pytest.raises(ValueError, match="32 bits"):
+        ckv.ckv_paged_plan(ints[:3], ints[:3], ints.view(3, 3), 16 + over, ints, one, ints[:4], ints[:3], ints, one)
+    q, k = torch.zeros(9, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 9, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="cu_seqlens"):
+        ckv.ckv_prefill_attention(desc, q, k, k, [0, 4 + over, 9], torch.empty_like(q))
