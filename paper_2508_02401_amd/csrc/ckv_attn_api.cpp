@@ -117,14 +117,14 @@ struct PagedSpace {
 };
 PagedSpace paged_space(const ckv_attn_desc* d, const ckv_paged_batch* b) {
   const int64_t rows = (int64_t)b->max_q * (d->num_q_heads / d->num_kv_heads);
-  const size_t row = (size_t)(d->head_dim + 2) * sizeof(float);
+  auto slot = [&](int64_t n) { return (size_t)ckv::partial_words((int32_t)n, d->head_dim) * sizeof(float); };
   PagedSpace s = {};
   if (b->max_kv > ckv::kFewLeast) {
     s.few_slots = 2 * ckv::kFewRounds * few_target(d);
-    s.few = s.few_slots * std::min<int64_t>(rows, ckv::kFewRows) * row;
+    s.few = s.few_slots * slot(std::min<int64_t>(rows, ckv::kFewRows));
     s.notes = (size_t)b->total_q * d->num_q_heads * sizeof(ckv::RowNote);
   }
-  if (rows > ckv::kFewRows && b->max_kv > ckv::kManyLeast) s.many = (size_t)kManyTarget * ckv::kAttnRows * row;
+  if (rows > ckv::kFewRows && b->max_kv > ckv::kManyLeast) s.many = (size_t)kManyTarget * slot(ckv::kAttnRows);
   return s;
 }
 

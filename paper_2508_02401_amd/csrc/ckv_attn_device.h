@@ -302,10 +302,10 @@ __device__ __forceinline__ float part_weight(float2 x, float m) {
 // Partial results of a split item, in its slot: `rows` rows of D floats, then
 // their (maximum, sum) pairs.
 __device__ __forceinline__ float* partial_o(float* part, int64_t slot, int rows, int D) {
-  return part + slot * rows * (D + 2);
+  return part + slot * partial_words(rows, D);
 }
 __device__ __forceinline__ float2* partial_ml(float* part, int64_t slot, int rows, int D) {
-  return reinterpret_cast<float2*>(part + slot * rows * (D + 2) + rows * D);
+  return reinterpret_cast<float2*>(partial_o(part, slot, rows, D) + rows * D);
 }
 
 __device__ __forceinline__ RowNote row_note(int64_t slot, int n_chunks, int row, bool many) {

@@ -392,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void paged_merge_kernel(const PagedArgs A
   // what it holds that is not finite reaches the row.
   auto gather = [&](const RowNote x, int first, int stride, float& m, float& l, float4& acc) {
     const int rows = x.many() ? kAttnRows : A.few_rows, step = x.many() ? a.n_kv : 1, n = x.n(), row = x.row();
-    const int64_t words = (int64_t)rows * (D + 2);
+    const int64_t words = partial_words(rows, D);
     const float* part = (x.many() ? A.part_many : A.part) + x.slot() * words;
     m = -INFINITY;
     l = 0.f;

@@ -156,6 +156,13 @@ inline PageDiv page_div(int32_t size) {
   return PageDiv{(uint32_t)((num + size - 1) / size), 31 + s};
 }
 
+// Floats of a slot for a split item's partial result: `rows` rows of d, then their (maximum,
+// sum) pairs. Whole 16 bytes, which the rows are written and read in: an odd number of
+// pairs leaves 8 over.
+constexpr int64_t partial_words(int32_t rows, int32_t d) {
+  return (int64_t)rows * d + (2 * (int64_t)rows + 3) / 4 * 4;
+}
+
 // Chunks of up to `chunk` keys that a request's n are cut into; one where it has none, as its
 // rows are written all the same. n reaches CKV_MAX_PAGED_KV: n + chunk would pass 2^31.
 constexpr int32_t paged_chunks(int32_t n, int32_t chunk) { return n <= chunk ? 1 : 1 + (n - 1) / chunk; }
