@@ -1,5 +1,5 @@
-// Device helpers of the attention kernels: waits, operand rounding, values that
-// are not finite, and how a paged batch is cut into workgroups.
+// Device helpers of the attention and decode kernels: waits, operand rounding, values
+// that are not finite, and how a paged batch is cut into workgroups.
 #pragma once
 
 #include "ckv_device.h"
@@ -29,8 +29,9 @@ __device__ __forceinline__ void barrier() {
 constexpr float kF16Bias = 8.f;
 constexpr float kSlack = 6.f;
 
-// exp2 of a logit's distance to the maximum. fp32 keeps weights below 2^-126,
-// which the bare instruction flushes to zero.
+// exp2 of a logit's distance to the maximum. fp32 caches keep weights below
+// 2^-126, which the bare instruction flushes to zero; V may be that large. The
+// 16-bit types' weights are rounded to operands that end sooner.
 template <int DT>
 __device__ __forceinline__ float weight_exp2(float x) {
   return DT == 2 ? exp2f(x) : fast_exp2(x);
@@ -49,6 +50,34 @@ __device__ __forceinline__ uint4 round_chunk(const float* x) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (_Float16)x[i];
     return __builtin_bit_cast(uint4, v);
+  }
+}
+
+// 8 (16-bit) or 4 (fp32) fp32 values -> one operand chunk, and for 16-bit types
+// the chunk of the rounded remainders.
+template <int DT>
+__device__ __forceinline__ void split_chunk(const float* x, uint4& hi, uint4& lo) {
+  if constexpr (DT == 2) {
+    hi = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                    __float_as_uint(x[3]));
+  } else if constexpr (DT == 0) {
+    bf16x8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      h[i] = (__bf16)x[i];
+      l[i] = (__bf16)(x[i] - (float)h[i]);
+    }
+    hi = __builtin_bit_cast(uint4, h);
+    lo = __builtin_bit_cast(uint4, l);
+  } else {
+    f16x8 h, l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      h[i] = (_Float16)x[i];
+      l[i] = (_Float16)(x[i] - (float)h[i]);
+    }
+    hi = __builtin_bit_cast(uint4, h);
+    lo = __builtin_bit_cast(uint4, l);
   }
 }
 

@@ -24,7 +24,7 @@
 // with the probabilities split into high and low parts.
 #include <math.h>
 
-#include "ckv_device.h"
+#include "ckv_attn_device.h"
 
 namespace ckv {
 namespace {
@@ -33,10 +33,6 @@ using namespace dev;
 
 constexpr int kDecThreads = kDecodeThreads;
 constexpr int kDecWaves = kDecThreads / 64;
-
-__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
-}
 
 template <int DT>
 __device__ __forceinline__ float elt_load(const void* base, int64_t i) {
@@ -220,34 +216,6 @@ __global__ __launch_bounds__(kDecThreads) void decode_rows_kernel_f32(const Deco
     for (int v = 0; v < 16; ++v) part[nb * 32 + acc_row(v, h)] = o[nb][v];
 }
 
-// 8 (16-bit) or 4 (fp32) fp32 values -> one operand chunk, and for 16-bit types
-// the chunk of the rounded remainders.
-template <int DT>
-__device__ __forceinline__ void split_chunk(const float* x, uint4& hi, uint4& lo) {
-  if constexpr (DT == 2) {
-    hi = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
-                    __float_as_uint(x[3]));
-  } else if constexpr (DT == 0) {
-    bf16x8 h, l;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      h[i] = (__bf16)x[i];
-      l[i] = (__bf16)(x[i] - (float)h[i]);
-    }
-    hi = __builtin_bit_cast(uint4, h);
-    lo = __builtin_bit_cast(uint4, l);
-  } else {
-    f16x8 h, l;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      h[i] = (_Float16)x[i];
-      l[i] = (_Float16)(x[i] - (float)h[i]);
-    }
-    hi = __builtin_bit_cast(uint4, h);
-    lo = __builtin_bit_cast(uint4, l);
-  }
-}
-
 // 16-bit inputs (bf16, f16): the same decode with 16-bit MFMA (32x32x16) at
 // fp32-level accuracy. Q, K and V are exact in the MFMA type; the
 // probabilities are split into a high part (rounded to the type) and a low
@@ -417,25 +385,6 @@ void decode_rows_kernel_16(const DecodeBatch B) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) part[nb * 32 + acc_row(v, h)] = o[nb][v];
 }
-
-// Wait until at most n vector-memory operations of this wave are outstanding
-// and its LDS operations are done; nothing is moved across.
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x070 | (N & 15) | ((N >> 4) << 14));
-  asm volatile("" ::: "memory");
-}
-
-// exp2 of a logit's distance to the maximum. fp32 caches keep weights below
-// 2^-126, which the bare instruction flushes to zero; V may be that large. The
-// 16-bit types' weights are rounded to high and low parts that end sooner.
-template <int DT>
-__device__ __forceinline__ float weight_exp2(float x) {
-  return DT == 2 ? exp2f(x) : fast_exp2(x);
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // Up to 32 * NQ query rows. A cache row is read once, so the bound is the
 // stream: what counts is how much of it is in flight and that no wave waits
