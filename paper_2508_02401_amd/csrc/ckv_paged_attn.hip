@@ -6,9 +6,14 @@
 //   workgroup per (request, KV head, chunk of its keys) or per (prompt, KV head,
 //   row tile). The keys go round the waves, which need no barrier between them:
 //   every wave owns 32-key tiles, whose K and V go from memory straight into the
-//   wave's part of LDS, the next tile's K requested as soon as this one's is in
-//   registers (the same for V). The waves' results meet in LDS. Over a cache each
-//   row is read once, so the bound is the stream; a prompt's come from L2.
+//   wave's part of LDS. The waves' results meet in LDS. Over a cache each row is
+//   read once, so the bound is the stream, and a prompt's rows come from L2.
+//   The next tile's K (V) is requested once this one's is in registers, and a tile starts
+//   when both are there. In 16-bit types the next K does not stay open over the reads of
+//   V: the compiler, which cannot tell the parts of LDS apart, waits for it there, as it
+//   waits for the page numbers read ahead over a cache. Counted waits, which let a tile
+//   start on K while V is on the way, took the same time: what keeps the stream up are
+//   the CU's other waves.
 // paged_merge_kernel: the chunks' partial results (of this kernel and of the tile
 //   kernel) rescaled to the common maximum and added in order.
 #include <math.h>
@@ -185,7 +190,7 @@ void few_kernel(const Args A) {
 
   for (; tile < nt; tile += kWaves) {
     const bool more = tile + kWaves < nt;
-    wait_vm<PT>();  // this tile's K; its V may still be on the way
+    wait_vm<0>();  // this tile's K and V
     uint4 kr[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) kr[c] = kl[wave][l32 * NV + ((2 * c + h) ^ swz(l32))];
@@ -227,8 +232,6 @@ void few_kernel(const Args A) {
       psum += s[v];
     }
     l_run += psum;
-    if (more) wait_vm<PT>();  // this tile's V; the next K may still be on the way
-    else wait_vm<0>();
     if (vis != ~0u) {  // keys that are not there count as zeros
 #pragma unroll
       for (int i = 0; i < PT; ++i)
