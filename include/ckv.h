@@ -381,7 +381,8 @@ int ckv_normalize_errors(const double *e, int32_t n_sets, int32_t n_layers, doub
  * attention of new tokens over it. They share ckv_attn_desc; outputs have the
  * descriptor's dtype, everything accumulates in fp32. Weights of 16-bit types
  * are rounded once to that type for the product with V, after the maximum (or
- * a number at most 2^8 below it) was divided out; their sum is taken before.
+ * a number below it, by up to 2^6 in bf16 and 2^14 in f16) was divided out;
+ * their sum is taken before.
  * A NaN or an infinity in a key or value reaches the rows that see it and no
  * other. All work is asynchronous on stream, makes no allocation, and may be
  * captured into a graph. */
