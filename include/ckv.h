@@ -380,9 +380,12 @@ int ckv_normalize_errors(const double *e, int32_t n_sets, int32_t n_layers, doub
  * paged cache that takes the compact rows and the tokens after them, and the
  * attention of new tokens over it. They share ckv_attn_desc; outputs have the
  * descriptor's dtype, everything accumulates in fp32. Weights of 16-bit types
- * are rounded once to that type for the product with V, after the maximum (or
- * a number below it, by up to 2^6 in bf16 and 2^14 in f16) was divided out;
- * their sum is taken before.
+ * are taken against the row's maximum, or a number below it (by up to 2^6 in bf16
+ * and 2^14 in f16), and rounded to that type for the product with V, while their
+ * sum is taken before: once in ckv_prefill_attention, and in ckv_paged_attention
+ * for requests of more than 32 rows per KV head (new tokens times H / n_kv); to
+ * high and low parts, as in ckv_decode_attention, for those of up to 32. A batch
+ * of one request goes by its bound, max_q.
  * A NaN or an infinity in a key or value reaches the rows that see it and no
  * other. All work is asynchronous on stream, makes no allocation, and may be
  * captured into a graph. */

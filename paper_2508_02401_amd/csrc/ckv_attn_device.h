@@ -99,6 +99,22 @@ __device__ __forceinline__ uint4 strip_chunk(uint4 v, uint4& x) {
   x = round_chunk<DT>(f);
   return __builtin_bit_cast(uint4, a);
 }
+// acc and 0 times the chunk's values: NaN where one of them is not finite.
+template <int DT>
+__device__ __forceinline__ float zero_times(uint4 v, float acc) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == 0) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), bf16x2{0, 0}, acc, false);
+    } else {
+      typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+      acc = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w[i]), f16x2{0, 0}, acc, false);
+    }
+  }
+  return acc;
+}
 __device__ __forceinline__ float strip_f32(float v, float& x) {
   x = fabsf(v) < INFINITY ? 0.f : v == INFINITY ? kPlusInf : v == -INFINITY ? kMinusInf : kNan;
   return fabsf(v) < INFINITY ? v : 0.f;

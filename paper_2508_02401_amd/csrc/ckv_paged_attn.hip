@@ -241,7 +241,8 @@ void few_kernel(const Args A) {
     const char* vt = reinterpret_cast<const char*>(vl[wave]);
     // A hidden key's weight is 0, but 0 times a value that is not finite is not:
     // where keys are hidden such values are left out of the product, and what a
-    // row sees of them is added.
+    // row sees of them is added; likewise where a weight's low part, of either sign
+    // or 0, would make a NaN of an infinity.
     if constexpr (DT != 2) {
       // P^T operands: MFMA step m takes this lane's keys acc_row(8m .. 8m+7, h)
       // = 16m + 4h + (0..3) and 16m + 8 + 4h + (0..3), in that order
@@ -252,15 +253,30 @@ void few_kernel(const Args A) {
         for (int nb = 0; nb < NB; ++nb) vr[m][nb] = v_chunk(vt, nb, m);
       wait_vm<63>();  // V is in registers
       if (more) fetch(vbase, tile + kWaves, page, vl[wave], vswz);
-      uint4 ph[2];
+      // A cache's weights keep a high and a low part, as ckv_decode_attention's do: its rows
+      // are few and the stream bounds it (64 single tokens 82.9 us with both, 81.9 rounded
+      // once), and the outputs are as exact as their type (rounded once they were 1.3 to 1.4
+      // times as far off). A prompt's are rounded once, in either kernel: both parts took
+      // 5% longer here and 35% in the large tiles.
+      uint4 ph[2], pl[2];
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = s[8 * m + i];
-        ph[m] = round_chunk<DT>(p);
+        if constexpr (PAGED) split_chunk<DT>(p, ph[m], pl[m]);
+        else ph[m] = round_chunk<DT>(p);
       }
-      if (hides) {
+      bool strip = hides;
+      if constexpr (PAGED) {
+        float zero = 0.f;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) zero = zero_times<DT>(vr[m][nb], zero);
+        strip = strip || __any(zero != 0.f);
+      }
+      if (strip) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           f32x16 c = f32x16{};
@@ -277,7 +293,10 @@ void few_kernel(const Args A) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) o[nb] = mfma_chunk<DT>(vr[m][nb], ph[m], o[nb]);
+        for (int nb = 0; nb < NB; ++nb) {
+          o[nb] = mfma_chunk<DT>(vr[m][nb], ph[m], o[nb]);
+          if constexpr (PAGED) o[nb] = mfma_chunk<DT>(vr[m][nb], pl[m], o[nb]);
+        }
     } else {
       float vr[16][NB];
 #pragma unroll
