@@ -96,18 +96,6 @@ int32_t few_target(const ckv_attn_desc* d) {
 }
 constexpr int32_t kManyTarget = ckv::kCUs;  // and of the tile kernel
 
-// Prompts of up to this many tiles of kAttnRows rows, over all KV heads, take tiles of
-// kFewRows with the keys shared out to the waves: large tiles would leave CUs empty, small
-// ones read K and V again for every 32 rows. Large against small, in us:
-//   head dim 64:  bf16 64 tiles 45 / 21, 256 tiles 86 / 80, 376 tiles 127 / 154;
-//                 fp32 64 tiles 281 / 77, 256 tiles 562 / 367
-//   head dim 128: bf16 64 tiles 25 / 17, 128 tiles 42 / 39, 192 tiles 55 / 62;
-//                 fp32 128 tiles 261 / 152, 192 tiles 372 / 279, but four prompts of
-//                 160 tiles in all 85 / 113
-int64_t prefill_few_tiles(const ckv_attn_desc* d) {
-  return d->head_dim == 64 ? ckv::kCUs : d->dtype == CKV_F32 ? ckv::kCUs * 3 / 4 : ckv::kCUs / 2;
-}
-
 // What a batch of these bounds needs of the workspace: partial results of requests
 // of few rows (slots for twice kFewRounds rounds, as a split request has two chunks
 // at least) and of the tile kernel (one round), and a note per row.
@@ -165,12 +153,9 @@ int ckv_prefill_attention(const ckv_attn_desc* desc, const ckv_packed_attn* a,
     const int32_t n = p.n;
     auto len = [&](int32_t i) { return cu[i + 1] - cu[i]; };
     int32_t longest = 0;
-    int64_t tiles = 0;
-    for (int32_t i = 0; i < n; ++i) {
-      longest = std::max(longest, len(i));
-      tiles += ceil_div(len(i) * G, ckv::kAttnRows);
-    }
-    const bool few = tiles * desc->num_kv_heads <= prefill_few_tiles(desc);
+    for (int32_t i = 0; i < n; ++i) longest = std::max(longest, len(i));
+    const bool few = ckv::prefill_small_tiles(desc->dtype == CKV_F32, desc->head_dim, ckv::kCUs, ckv::kFewRows, G,
+                                              desc->num_kv_heads, cu, n);
     const int64_t rows_per = few ? ckv::kFewRows : ckv::kAttnRows;
     // A tile's work is its last row's position. Tiles run from long to short, in
     // bands of position over all prompts, so that no long one starts when the others

@@ -142,6 +142,35 @@ inline int64_t deal_unit_parts(int64_t cus, int32_t num_seqs, int32_t n_sg, int3
   return most;
 }
 
+// Whether n packed prompts (prompt i is rows cu[i] .. cu[i + 1]) take row tiles of `small` rows,
+// with the keys shared out to a workgroup's waves, or large ones. Large tiles end with the
+// longest prompt's last one, which walks all its keys on one CU whatever the others do; small
+// ones have that much shorter a chain, but read K and V again for every `small` rows and
+// each pay their start and end. So small ones are taken while their work per CU, with 384 keys
+// for start and end of each, is at most `ratio` times the longest prompt. Large / small, in us,
+// on both sides, 32 heads over 8:
+//   64, 16 bits    one prompt of 1536 tokens 36 / 33, of 2560 58 / 67; four of 320 13 / 20
+//   64, fp32       one of 2560 353 / 293, of 4096 603 / 701; four of 256 41 / 34, of 640 95 / 114
+//   128, 16 bits   one of 512 23 / 17, of 1280 44 / 51; four of 320 19 / 39
+//   128, fp32      one of 2048 515 / 458, of 2560 642 / 672; four of 146 48 / 42 (28 heads
+//                  over 4), of 320 87 / 115
+// Of 424 sets of 1, 4 and 16 prompts, even and uneven, the other tiles would have been 7% faster
+// at most, and of 150 random sets 20% at most, 0.8% on average (with a bound on the number
+// of tiles, which is not what decides, 170% and 90%, 3.9%).
+inline bool prefill_small_tiles(bool f32, int32_t head_dim, int64_t cus, int32_t small, int64_t G, int64_t n_kv,
+                                const int32_t* cu, int32_t n) {
+  const double ratio = head_dim == 64 ? (f32 ? 8.3 : 5.0) : (f32 ? 6.8 : 3.2);
+  double work = 0;
+  int32_t longest = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int32_t len = cu[i + 1] - cu[i];
+    const int64_t tiles = (len * G + small - 1) / small;
+    work += (double)tiles * ((len + 1) * 0.5 + 384);
+    longest = len > longest ? len : longest;
+  }
+  return work * (double)n_kv <= ratio * (double)cus * longest;
+}
+
 // Division of a token number (below 2^31) by the page size, as one multiply and
 // shift: with 2^(s-1) < size <= 2^s and mul = ceil(2^(31+s) / size), the error
 // mul * size - 2^(31+s) is below 2^s, so (x * mul) >> (31+s) is exact.
