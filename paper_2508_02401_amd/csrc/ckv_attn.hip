@@ -13,9 +13,9 @@
 //
 // What bounds it: a wave and tile of 64 keys (bf16, d 128) take 1024 cycles of the
 // matrix units and about 950 of the vector units (528 of them the 32 exponentials),
-// and the two waves of a SIMD hardly overlap the one with the other: 4400
-// cycles per tile of 256 rows. 32768 tokens of 32 heads over 8 take 8.2 ms,
-// 1.07 PFLOP/s, where a library product of 8192^3 reaches 1.22. Running the second
+// and the two waves of a SIMD hardly overlap the one with the other: 4200
+// cycles per tile of 256 rows. 32768 tokens of 32 heads over 8 take 8.2 to 8.6 ms
+// by the card, 1.02 to 1.07 PFLOP/s, where a library product of 8192^3 reaches 1.22. Running the second
 // four waves half a step behind the first, so that one half multiplies while
 // the other works out its weights, took 9.0 ms; alternating the two chains of
 // QK^T made no difference.
@@ -129,7 +129,7 @@ void attn_kernel(const Args A) {
   auto swz = [](int row) { return ROWB >= 256 ? (row & 15) : ((row >> 1) & 7); };
   // V of 16-bit types is read 4 keys of 64 bytes at a time, which meet every bank once if
   // they lie in different quarters of the 256 bytes (with K's swizzle, 59% of the LDS
-  // cycles were bank conflicts and a prompt of 32768 tokens took 8.6 ms, not 8.2);
+  // cycles were bank conflicts and a prompt of 8192 tokens took 574 us, not 542);
   // rows of fp32 are read along their columns, which does as it is
   auto vswz = [&](int row) { return DT == 2 ? 0 : ROWB >= 256 ? (row & 3) * 4 : (row & 2) * 2; };
   const int lrow = lane / NV, lpos = lane % NV;
@@ -286,6 +286,9 @@ void attn_kernel(const Args A) {
   };
   // P^T operands: MFMA step km takes this lane's keys acc_row(8km .. 8km+7, h)
   // = 16km + 4h + (0..3) and 16km + 8 + 4h + (0..3), in that order
+  // Rounded once to the type: a second product for the rounding's remainders took 12.0 ms
+  // in place of 8.6 for 32768 tokens and 775 us in place of 562 for 8192, and brought the
+  // relative error of bf16 outputs from 2.1e-3 to the 1.6e-3 of their own rounding
   auto p_chunk = [&](const f32x16 (&s)[KB], int km) {
     float p[8];
 #pragma unroll

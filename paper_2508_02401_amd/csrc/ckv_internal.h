@@ -354,7 +354,7 @@ constexpr int kFewRows = 32;     // rows per KV head of the kernel for few
 constexpr int kFewLeast = 128;   // keys per workgroup, at least
 constexpr int kManyLeast = 1024;
 // Rounds of shares where there are many requests: 64 requests of 64 to 8192 tokens, 8 KV
-// heads, take 97 / 90 / 95 us with 2 / 3 / 4 (small shares end together, but each costs
+// heads, take 92 / 83 / 87 us with 2 / 3 / 4 (small shares end together, but each costs
 // its own start)
 constexpr int kFewRounds = 3;
 
