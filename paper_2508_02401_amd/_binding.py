@@ -738,6 +738,8 @@ def ckv_paged_attention(desc: ckv_attn_desc, cache: ckv_paged_cache, batch: ckv_
     a = _rows_arg(what, desc, q, out, lse)
     if q.shape[0] < batch.total_q:
         raise ValueError("%s: fewer rows than total_q" % what)
+    if not workspace.is_contiguous():
+        raise ValueError("%s: workspace must be contiguous" % what)
     dev = _on_device(what, q, out, ck, workspace, lse, *_tensors(what, batch, "paged_batch"))
     _call_on(dev, load().ckv_paged_attention, what,
              (ctypes.byref(desc), ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(a),

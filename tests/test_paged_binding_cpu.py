@@ -46,3 +46,13 @@ def test_numbers_past_32_bits(over):
     q, k = torch.zeros(9, 4, 64, dtype=torch.bfloat16), torch.zeros(2, 9, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="cu_seqlens"):
         ckv.ckv_prefill_attention(desc, q, k, k, [0, 4 + over, 9], torch.empty_like(q))
+
+
+def test_workspaces_with_gaps():
+    # its bytes are counted, and written one after the other from its first on
+    desc, pool, ints = ckv.attn_desc(4, 2, 64), _pool(), torch.zeros(9, dtype=torch.int32)
+    cache, batch = ckv.paged_cache(pool, pool), ckv.paged_batch(ints[:4], ints[:3], ints.view(3, 3), 9, 4, 9)
+    q = torch.zeros(9, 4, 64, dtype=torch.bfloat16)
+    for ws in (torch.zeros(1).expand(10 ** 6), torch.zeros(2 * 10 ** 5)[::2]):
+        with pytest.raises(ValueError, match="contiguous"):
+            ckv.ckv_paged_attention(desc, cache, batch, q, torch.empty_like(q), ws)
